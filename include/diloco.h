@@ -475,6 +475,152 @@ typedef struct {
 int diloco_compute_utilization(const diloco_cu_input_t *in, diloco_cu_output_t *out);
 double diloco_bandwidth_for_utilization(const diloco_cu_input_t *in, double target_utilization);
 
+/*
+ * OPERATORS OF THE INNER STEP'S DECODER.  The inner phase trains a decoder on every replica
+ * (Section 3, Table 5: QKNorm, z-loss, vocabulary 32 000); besides its matrix products it needs
+ * the four operators below, each with its gradient, so that what diloco_inner_adamw takes as
+ * grads is produced on the same device by the same library.  Operators with parameters read
+ * them in place from the replicas' flat vectors and write their gradients in place into the
+ * flat gradients: a parameter argument is the address of replica 0's first element, and its
+ * stride is the distance in elements to the next replica's (the state's stride / grad_stride),
+ * all M replicas in one call.
+ *
+ * Rules of this part, where they differ from the general ones above
+ *   - no state handle: sizes, strides and types come in a descriptor (host memory, read during
+ *     the call), tensors as device pointers on the current device (a host pointer is refused).
+ *   - strides are in elements, >= 0 and such that no two elements of an output coincide; the last
+ *     axis is contiguous.  Base pointers are aligned to their element.  16-byte aligned rows
+ *     are faster; nothing else depends on it except where a call says so.
+ *   - arithmetic: fp32 (sums, softmax statistics and gradients of parameters included), with FMA
+ *     contraction; bf16 is a storage type of tensors, and the operand type of the attention's matrix
+ *     products.  Every result is rounded once, on the way out.  Results do not depend on the
+ *     launch and are the same bits from call to call: no floating-point atomics.
+ *   - a call whose output is empty (no rows, no tokens) returns DILOCO_OK and launches only what
+ *     the outputs that remain need.
+ *   - a workspace is device memory of the caller, 256-byte aligned, contents irrelevant on entry and
+ *     undefined afterwards; two calls that may overlap on the GPU need two.
+ *   - all of them may be captured in CUDA graphs.
+ * Errors of every call: INVALID_ARG (null or host pointer, negative size, bad type or stride, workspace
+ * too small), MISALIGNED, UNSUPPORTED (a size beyond the limit its call states), CUDA.
+ */
+enum { DILOCO_DTYPE_F32 = 0, DILOCO_DTYPE_BF16 = 1 };
+
+/*
+ * EMBEDDING LOOKUP WITH SCALING, out[m, t, :] = scale * table[m, ids[m, t], :], and its gradient
+ *   dtable[m, v, :] = scale * sum over t with ids[m, t] = v of dout[m, t, :]   (+ dtable, if accumulate).
+ * An id outside [0, vocab) stands for no token: its output row is zero, it takes no part in the gradient.
+ * backward sorts each replica's tokens by id (stable) and sums each row's terms in fp32 in an order that
+ * depends on the ids alone.  accumulate = 0 writes every row of dtable (zero for ids that do not
+ * appear), accumulate != 0 touches only rows that appear: the form for a table that is also the output
+ * projection, whose dense gradient is already there.  vocab <= 2^20, M * tokens < 2^31.
+ * The workspace's size is diloco_embedding_workspace_bytes (negative: a status).
+ */
+typedef struct {
+  int32_t M;            /* replicas                                                                    */
+  int32_t d;            /* elements of a row                                                           */
+  int64_t tokens;       /* tokens of each replica; ids are [M, tokens] contiguous                      */
+  int64_t vocab;        /* rows of the table, contiguous: [vocab, d] at every replica                  */
+  int64_t table_stride; /* elements from one replica's table to the next one's                         */
+  int64_t grad_stride;  /* the same for dtable                                                         */
+  int64_t row_stride;   /* elements from one token's row of out / dout to the next; replicas follow on */
+  float scale;
+  int32_t ids_int64;    /* 0: ids are int32, 1: int64                                                  */
+  int32_t table_dtype, act_dtype, grad_dtype; /* DILOCO_DTYPE_* of table, out and dout, dtable           */
+} diloco_embedding_t;
+int diloco_embedding_forward(const diloco_embedding_t *e, const void *ids, const void *table, void *out, void *cuda_stream);
+int64_t diloco_embedding_workspace_bytes(const diloco_embedding_t *e);
+int diloco_embedding_backward(const diloco_embedding_t *e, const void *ids, const void *dout, void *dtable,
+                              int32_t accumulate, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/*
+ * LAYER NORM of vectors of d elements, x[m, r, g, :] for replica m, row r and group g (groups = 1: the
+ * norm over the model width; groups = heads: QKNorm, one weight for all heads):
+ *   mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),  xh = (x - mean) rstd,
+ *   y = weight xh + bias
+ *   dx = rstd (w dy - sum(w dy) / d - xh sum(w dy xh) / d),
+ *   dweight = sum over rows and groups of dy xh,  dbias = sum of dy          (+ their old values, if accumulate).
+ * mean and rstd are fp32, [M, rows, groups] contiguous; forward writes them where they are not NULL, backward
+ * reads them.  Vector (r, g) of replica m starts at (m rows + r) row_stride + g group_stride of its tensor, so q
+ * and k are normalised in place inside a fused projection's rows.  bias and dbias may be NULL; backward may be
+ * called without dweight and dbias.  y may be x and dx may be dy (same strides).  d <= 65536.
+ */
+typedef struct {
+  int32_t M, d, groups;
+  int64_t rows;                          /* rows of each replica                                         */
+  int64_t x_row_stride, x_group_stride;
+  int64_t y_row_stride, y_group_stride;   /* of y in forward, of dy in backward                           */
+  int64_t dx_row_stride, dx_group_stride; /* backward only                                                */
+  int64_t param_stride;                  /* elements from one replica's weight (bias) to the next one's  */
+  int64_t grad_stride;                   /* the same for dweight (dbias)                                 */
+  float eps;
+  int32_t act_dtype, param_dtype, grad_dtype; /* of x, y, dy, dx; of weight, bias; of dweight, dbias        */
+} diloco_layernorm_t;
+int diloco_layernorm_forward(const diloco_layernorm_t *n, const void *x, const void *weight, const void *bias, void *y,
+                             float *mean, float *rstd, void *cuda_stream);
+int64_t diloco_layernorm_workspace_bytes(const diloco_layernorm_t *n);
+int diloco_layernorm_backward(const diloco_layernorm_t *n, const void *dy, const void *x, const void *weight,
+                              const float *mean, const float *rstd, void *dx, void *dweight, void *dbias, int32_t accumulate,
+                              void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/*
+ * CAUSAL ATTENTION OVER PACKED SEQUENCES, grouped heads.  tokens rows hold `sequences` whole sequences one
+ * after another, sequence b = rows [cu_seqlens[b], cu_seqlens[b+1]) (device memory, int32, sequences + 1 values, not
+ * decreasing, from 0 to at most tokens); an empty sequence is allowed.  Head h of q reads head
+ * g = h / (heads / kv_heads) of k and v.  With i, j rows of one sequence, j <= i:
+ *   z_ij = scale q_i . k_j,  lse_i = log sum_j exp(z_ij),  P_ij = exp(z_ij - lse_i),  out_i = sum_j P_ij v_j
+ *   dv_j = sum_{h of g} sum_i P_ij dout_i,   dz_ij = P_ij (dout_i . v_j - delta_i),  delta_i = dout_i . out_i,
+ *   dq_i = scale sum_j dz_ij k_j,   dk_j = scale sum_{h of g} sum_i dz_ij q_i.
+ * Rows that belong to no sequence (from cu_seqlens[sequences] on) get out = 0, lse = -infinity and zero
+ * gradients, whatever they hold.  Keys that a row does not see never reach it, even if they are infinite or NaN.
+ * All tensors bf16 except lse, fp32 [heads, tokens]; row i of head h of a tensor starts at i row_stride + h
+ * head_stride.  head_dim is a multiple of 8, at most 128 (64 and less run narrower kernels); base pointers 16-byte
+ * aligned, strides multiples of 8 elements (MISALIGNED otherwise).  tokens <= 2^24, sequences <= 2^20, heads <= 65535.
+ * P and dz are rounded to bf16 as operands of the second products; every sum is fp32.
+ * device_status as in diloco_buffers_t: one word or NULL.  Every wait of these kernels is bounded (1 s); one that
+ * runs out sets the word (diloco_check_status_word), and the results of that call are invalid.
+ */
+typedef struct {
+  int32_t heads, kv_heads, head_dim, sequences;
+  int64_t tokens;
+  int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int64_t o_row_stride, o_head_stride;       /* of out                                                  */
+  int64_t do_row_stride, do_head_stride;     /* these and the following: backward only                  */
+  int64_t dq_row_stride, dq_head_stride, dk_row_stride, dk_head_stride, dv_row_stride, dv_head_stride;
+  float scale;
+  uint32_t *device_status;
+} diloco_attention_t;
+int diloco_attention_forward(const diloco_attention_t *a, const void *q, const void *k, const void *v,
+                             const int32_t *cu_seqlens, void *out, float *lse, void *cuda_stream);
+int64_t diloco_attention_workspace_bytes(const diloco_attention_t *a); /* of backward */
+int diloco_attention_backward(const diloco_attention_t *a, const void *dout, const void *q, const void *k, const void *v,
+                              const void *out, const float *lse, const int32_t *cu_seqlens, void *dq, void *dk, void *dv,
+                              void *workspace, int64_t workspace_bytes, void *cuda_stream);
+/* Reads a status word as diloco_check_device_status does (synchronises the stream); NULL is OK. */
+int diloco_check_status_word(const uint32_t *device_status, void *cuda_stream);
+
+/*
+ * DISTILLATION FROM A TEACHER'S TOP LOGITS, with z-loss.  Row n has student logits x[n, 0 .. vocab) and up to k
+ * teacher entries (id, logit t); an id outside [0, vocab) marks an unused entry.  With temperature T:
+ *   lse = log sum_v exp(x_v / T),  p = softmax over the used entries of t / T,
+ *   loss = w (T^2 sum_k p_k (log p_k - (x_{id_k} / T - lse)) + z_coef lse^2),
+ *   dx_v = w (T (exp(x_v / T - lse) - sum_{k: id_k = v} p_k) + 2 z_coef lse exp(x_v / T - lse) / T),
+ * w = grad_scale row_weight[n] (row_weight NULL: 1).  A row without used entries has loss 0 and dx 0; its lse is
+ * still written.  k = 1 and T = 1 is the cross-entropy of a target token, whatever its teacher logit.  Gradients of
+ * the teacher are not formed.  An id may appear more than once.  loss and lse are fp32 [rows], dlogits (NULL: loss only) has
+ * the logits' type and may be the logits themselves (same stride).  teacher ids [rows, k] int32 or
+ * int64, teacher logits [rows, k], both contiguous.  1 <= k <= 1024, vocab < 2^31.
+ */
+typedef struct {
+  int64_t rows, vocab;
+  int64_t logits_stride, grad_stride;
+  int32_t k;
+  int32_t ids_int64;
+  int32_t dtype, teacher_dtype;
+  float temperature, z_coef, grad_scale;
+} diloco_distill_t;
+int diloco_distill_loss(const diloco_distill_t *l, const void *logits, const void *teacher_ids, const void *teacher_logits,
+                        const float *row_weight, float *loss, float *lse, void *dlogits, void *cuda_stream);
+
 /* Number of kernels this library has launched in this process so far. */
 int64_t diloco_launch_count(void);
 /* The raw cudaError_t of the last failed runtime call made by the library (0 if none). */

@@ -20,6 +20,7 @@ IMPL_AUTO, IMPL_DIRECT, IMPL_BULK, IMPL_SPLIT_R2, IMPL_SPLIT_R4 = 0, 1, 2, 3, 4
 IMPL_TENSOR_T256, IMPL_TENSOR_T128, IMPL_TENSOR_T64 = 5, 6, 7
 STANDARD, DELAYED, EAGER = 0, 1, 2
 COMM_F32, COMM_BF16, COMM_EXMY = 0, 1, 2
+DTYPE_F32, DTYPE_BF16 = 0, 1
 MAX_M = 64
 MAX_OVERLAP = 4
 
@@ -53,6 +54,39 @@ class CUOutput(ctypes.Structure):
     """diloco_cu_output_t"""
     _fields_ = [(n, ctypes.c_double) for n in ("wire_bits", "comm_time_s", "tolerated_latency_s", "exposed_comm_time_s",
                                                "compute_time_s", "compute_utilization")]
+
+
+def _fields(kinds):
+    """"name name ...: type" lines -> ctypes fields, in order."""
+    types = dict(i32=ctypes.c_int32, i64=ctypes.c_int64, f32=ctypes.c_float, ptr=ctypes.c_void_p)
+    return [(n, types[t]) for t, names in kinds for n in names.split()]
+
+
+class Embedding(ctypes.Structure):
+    """diloco_embedding_t"""
+    _fields_ = _fields([("i32", "M d"), ("i64", "tokens vocab table_stride grad_stride row_stride"), ("f32", "scale"),
+                        ("i32", "ids_int64 table_dtype act_dtype grad_dtype")])
+
+
+class LayerNorm(ctypes.Structure):
+    """diloco_layernorm_t"""
+    _fields_ = _fields([("i32", "M d groups"), ("i64", "rows x_row_stride x_group_stride y_row_stride y_group_stride "
+                        "dx_row_stride dx_group_stride param_stride grad_stride"), ("f32", "eps"),
+                        ("i32", "act_dtype param_dtype grad_dtype")])
+
+
+class Attention(ctypes.Structure):
+    """diloco_attention_t"""
+    _fields_ = _fields([("i32", "heads kv_heads head_dim sequences"),
+                        ("i64", "tokens " + " ".join(f"{t}_row_stride {t}_head_stride"
+                                                     for t in ("q", "k", "v", "o", "do", "dq", "dk", "dv"))),
+                        ("f32", "scale"), ("ptr", "device_status")])
+
+
+class Distill(ctypes.Structure):
+    """diloco_distill_t"""
+    _fields_ = _fields([("i64", "rows vocab logits_stride grad_stride"), ("i32", "k ids_int64 dtype teacher_dtype"),
+                        ("f32", "temperature z_coef grad_scale")])
 
 
 class DilocoError(RuntimeError):
@@ -95,6 +129,17 @@ SYMBOLS = {
     "diloco_check_device_status": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
     "diloco_compute_utilization": (ctypes.c_int, [ctypes.POINTER(CUInput), ctypes.POINTER(CUOutput)]),
     "diloco_bandwidth_for_utilization": (ctypes.c_double, [ctypes.POINTER(CUInput), ctypes.c_double]),
+    "diloco_embedding_forward": (ctypes.c_int, [ctypes.POINTER(Embedding)] + [ctypes.c_void_p] * 4),
+    "diloco_embedding_workspace_bytes": (ctypes.c_int64, [ctypes.POINTER(Embedding)]),
+    "diloco_embedding_backward": (ctypes.c_int, [ctypes.POINTER(Embedding)] + [ctypes.c_void_p] * 3 + [ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "diloco_layernorm_forward": (ctypes.c_int, [ctypes.POINTER(LayerNorm)] + [ctypes.c_void_p] * 7),
+    "diloco_layernorm_workspace_bytes": (ctypes.c_int64, [ctypes.POINTER(LayerNorm)]),
+    "diloco_layernorm_backward": (ctypes.c_int, [ctypes.POINTER(LayerNorm)] + [ctypes.c_void_p] * 8 + [ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "diloco_attention_forward": (ctypes.c_int, [ctypes.POINTER(Attention)] + [ctypes.c_void_p] * 7),
+    "diloco_attention_workspace_bytes": (ctypes.c_int64, [ctypes.POINTER(Attention)]),
+    "diloco_attention_backward": (ctypes.c_int, [ctypes.POINTER(Attention)] + [ctypes.c_void_p] * 11 + [ctypes.c_int64, ctypes.c_void_p]),
+    "diloco_check_status_word": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]),
+    "diloco_distill_loss": (ctypes.c_int, [ctypes.POINTER(Distill)] + [ctypes.c_void_p] * 8),
     "diloco_launch_count": (ctypes.c_int64, []),
     "diloco_last_cuda_error": (ctypes.c_int32, []),
     "diloco_status_string": (ctypes.c_char_p, [ctypes.c_int]),

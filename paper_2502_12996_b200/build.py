@@ -12,14 +12,17 @@ LIB = PKG / "libdiloco.so"
 REPORT = PKG / "ptxas_report.txt"        # registers / spills of every kernel, written by each build
 OUTER_M = [0, 1, 2, 3, 4, 8, 16, 1000, 1002, 1003, 1004]   # translation units: replica counts with kernels of their own, the
                                                  # warp-split forms (1000, 1002) and the first-steps form (0)
+OPERATORS = ["diloco_embedding", "diloco_layernorm", "diloco_distill", "diloco_attention"]   # units of the decoder operators
 OBJ = PKG / "_obj"
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-    "-fmad=false",                       # no FMA contraction: one rounding per operation
     "-prec-div=true", "-prec-sqrt=true", "-ftz=false",
     "-Xcompiler", "-fPIC", "-Xptxas", "-v",
 ] + os.environ.get("DILOCO_EXTRA_NVCC_FLAGS", "").split()
+
+
+STEP_FLAGS = ["-fmad=false"]             # the steps: no FMA contraction, one rounding per operation
 
 
 def _stale() -> bool:
@@ -30,8 +33,8 @@ def _stale() -> bool:
     return any(d.stat().st_mtime > t for d in deps)
 
 
-def _compile(nvcc: str, src: Path, obj: Path, defines) -> str:
-    cmd = [nvcc] + NVCC_FLAGS + [f"-D{d}" for d in defines] + ["-c", str(src), "-o", str(obj)]
+def _compile(nvcc: str, src: Path, obj: Path, flags) -> str:
+    cmd = [nvcc] + NVCC_FLAGS + list(flags) + ["-c", str(src), "-o", str(obj)]
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if res.returncode != 0:
         print(res.stdout)
@@ -40,15 +43,15 @@ def _compile(nvcc: str, src: Path, obj: Path, defines) -> str:
 
 
 def build_library(force: bool = False, verbose: bool = False) -> Path:
-    """Compile the host/ABI unit and one unit per replica count side by side, then link."""
+    """Compile the host/ABI unit, one unit per replica count and the operators side by side, then link."""
     if not force and not _stale() and REPORT.exists():
         return LIB
     from concurrent.futures import ThreadPoolExecutor
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     OBJ.mkdir(exist_ok=True)
-    jobs = [(CSRC / "diloco_api.cu", OBJ / "diloco_api.o", []),
-            (CSRC / "diloco_utilization.cu", OBJ / "diloco_utilization.o", [])]
-    jobs += [(CSRC / "diloco_outer_m.cu", OBJ / f"diloco_outer_m{m}.o", [f"DILOCO_M={m}"]) for m in OUTER_M]
+    jobs = [(CSRC / f"{n}.cu", OBJ / f"{n}.o", STEP_FLAGS) for n in ("diloco_api", "diloco_utilization")]
+    jobs += [(CSRC / "diloco_outer_m.cu", OBJ / f"diloco_outer_m{m}.o", STEP_FLAGS + [f"-DDILOCO_M={m}"]) for m in OUTER_M]
+    jobs += [(CSRC / f"{n}.cu", OBJ / f"{n}.o", []) for n in OPERATORS]
     with ThreadPoolExecutor(max_workers=min(len(jobs), os.cpu_count() or 1)) as pool:
         logs = list(pool.map(lambda j: _compile(nvcc, *j), jobs))
     tmp = LIB.with_suffix(f".so.tmp{os.getpid()}")

@@ -71,6 +71,20 @@ int diloco::cuda_fail(cudaError_t e) {
 }
 void diloco::count_launch() { g_launches.fetch_add(1); }
 
+// A pointer the kernels will dereference must be device (or managed) memory of `device`;
+// a host pointer here would otherwise surface as an illegal-address fault inside a kernel.
+int diloco::check_device_pointer(const void *p, int device) {
+  cudaPointerAttributes at;
+  cudaError_t e = cudaPointerGetAttributes(&at, p);
+  if (e != cudaSuccess) {
+    cudaGetLastError(); // clear the sticky-less error state of the query
+    return DILOCO_ERR_INVALID_ARG;
+  }
+  if (at.type == cudaMemoryTypeManaged) return DILOCO_OK;
+  if (at.type != cudaMemoryTypeDevice || at.device != device) return DILOCO_ERR_INVALID_ARG;
+  return DILOCO_OK;
+}
+
 namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -95,20 +109,6 @@ int validate_config(const diloco_config_t *c) {
   // 128-byte rows for every dtype in use
   if ((c->stride * 4) % 128 != 0) return DILOCO_ERR_MISALIGNED;
   if (c->theta_kind != DILOCO_THETA_F32 && (c->stride * 2) % 128 != 0) return DILOCO_ERR_MISALIGNED;
-  return DILOCO_OK;
-}
-
-// A pointer the kernels will dereference must be device (or managed) memory of `device`;
-// a host pointer here would otherwise surface as an illegal-address fault inside a kernel.
-int check_device_pointer(const void *p, int device) {
-  cudaPointerAttributes at;
-  cudaError_t e = cudaPointerGetAttributes(&at, p);
-  if (e != cudaSuccess) {
-    cudaGetLastError(); // clear the sticky-less error state of the query
-    return DILOCO_ERR_INVALID_ARG;
-  }
-  if (at.type == cudaMemoryTypeManaged) return DILOCO_OK;
-  if (at.type != cudaMemoryTypeDevice || at.device != device) return DILOCO_ERR_INVALID_ARG;
   return DILOCO_OK;
 }
 
@@ -1068,16 +1068,20 @@ int diloco_set_wait_limit(diloco_state_t *st, uint64_t limit_ns, uint32_t test_e
   return DILOCO_OK;
 }
 
-int diloco_check_device_status(diloco_state_t *st, void *stream) {
-  if (!st) return DILOCO_ERR_INVALID_ARG;
-  if (!st->buf.device_status) return DILOCO_OK;
+int diloco_check_status_word(const uint32_t *device_status, void *stream) {
+  if (!device_status) return DILOCO_OK;
   uint32_t word = 0;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = cudaMemcpyAsync(&word, st->buf.device_status, sizeof(word), cudaMemcpyDeviceToHost, s);
+  cudaError_t e = cudaMemcpyAsync(&word, device_status, sizeof(word), cudaMemcpyDeviceToHost, s);
   if (e != cudaSuccess) return cuda_fail(e);
   e = cudaStreamSynchronize(s);
   if (e != cudaSuccess) return cuda_fail(e);
   return word == 0 ? DILOCO_OK : DILOCO_ERR_DEVICE_TIMEOUT;
+}
+
+int diloco_check_device_status(diloco_state_t *st, void *stream) {
+  if (!st) return DILOCO_ERR_INVALID_ARG;
+  return diloco_check_status_word(st->buf.device_status, stream);
 }
 
 int64_t diloco_launch_count(void) { return g_launches.load(); }

@@ -1,0 +1,134 @@
+// Causal attention over packed sequences with grouped heads: host side, and the row-at-a-time kernels.
+#include "diloco_attention_rows.cuh"
+
+namespace diloco {
+namespace {
+
+constexpr int kRowWarps = 8;
+
+// One warp for each row (blockIdx.x * 8 + warp) of head blockIdx.y.
+__global__ void __launch_bounds__(32 * kRowWarps, 1) attn_forward_rows_kernel(const AttnArgs a) {
+  const int i = blockIdx.x * kRowWarps + (threadIdx.x >> 5), h = blockIdx.y, lane = threadIdx.x & 31;
+  if (i >= a.tokens) return;
+  int first, end;
+  sequence_of(a, i, first, end);
+  if (first >= 0) attn_out_row(a, i, h, first, lane);
+  else {
+    for (int c = lane; c < a.head_dim; c += 32) a.out[i * a.o_row + h * a.o_head + c] = __float2bfloat16_rn(0.f);
+    if (lane == 0) a.lse[(long long)h * a.tokens + i] = -INFINITY;
+  }
+}
+
+__global__ void __launch_bounds__(32 * kRowWarps, 1) attn_dq_rows_kernel(const AttnArgs a) {
+  const int i = blockIdx.x * kRowWarps + (threadIdx.x >> 5), h = blockIdx.y, lane = threadIdx.x & 31;
+  if (i >= a.tokens) return;
+  int first, end;
+  sequence_of(a, i, first, end);
+  if (first >= 0) attn_dq_row(a, i, h, first, lane);
+  else
+    for (int c = lane; c < a.head_dim; c += 32) a.dq[i * a.dq_row + h * a.dq_head + c] = __float2bfloat16_rn(0.f);
+}
+
+__global__ void __launch_bounds__(32 * kRowWarps, 1) attn_dkv_rows_kernel(const AttnArgs a) {
+  const int j = blockIdx.x * kRowWarps + (threadIdx.x >> 5), g = blockIdx.y, lane = threadIdx.x & 31;
+  if (j >= a.tokens) return;
+  int first, end;
+  sequence_of(a, j, first, end);
+  if (first >= 0) attn_dkv_row(a, j, g, end, lane);
+  else
+    for (int c = lane; c < a.head_dim; c += 32) {
+      a.dk[j * a.dk_row + g * a.dk_head + c] = __float2bfloat16_rn(0.f);
+      a.dv[j * a.dv_row + g * a.dv_head + c] = __float2bfloat16_rn(0.f);
+    }
+}
+
+bool stride_ok(int64_t row, int64_t head) { return row >= 0 && head >= 0; }
+bool stride_wide(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
+
+int valid(const diloco_attention_t *a, bool backward) {
+  if (!a) return DILOCO_ERR_INVALID_ARG;
+  if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads != 0 || a->head_dim < 1 || a->sequences < 0 || a->tokens < 0)
+    return DILOCO_ERR_INVALID_ARG;
+  if (!(a->scale > -INFINITY && a->scale < INFINITY)) return DILOCO_ERR_INVALID_ARG;
+  if (!stride_ok(a->q_row_stride, a->q_head_stride) || !stride_ok(a->k_row_stride, a->k_head_stride) ||
+      !stride_ok(a->v_row_stride, a->v_head_stride) || !stride_ok(a->o_row_stride, a->o_head_stride))
+    return DILOCO_ERR_INVALID_ARG;
+  if (backward && (!stride_ok(a->do_row_stride, a->do_head_stride) || !stride_ok(a->dq_row_stride, a->dq_head_stride) ||
+                   !stride_ok(a->dk_row_stride, a->dk_head_stride) || !stride_ok(a->dv_row_stride, a->dv_head_stride)))
+    return DILOCO_ERR_INVALID_ARG;
+  if (a->head_dim % 8 != 0 || a->head_dim > kMaxHeadDim || a->tokens > (1 << 24) || a->sequences > (1 << 20) || a->heads > 65535)
+    return DILOCO_ERR_UNSUPPORTED;
+  if (!stride_wide(a->q_row_stride, a->q_head_stride) || !stride_wide(a->k_row_stride, a->k_head_stride) ||
+      !stride_wide(a->v_row_stride, a->v_head_stride) || !stride_wide(a->o_row_stride, a->o_head_stride))
+    return DILOCO_ERR_MISALIGNED;
+  if (backward && (!stride_wide(a->do_row_stride, a->do_head_stride) || !stride_wide(a->dq_row_stride, a->dq_head_stride) ||
+                   !stride_wide(a->dk_row_stride, a->dk_head_stride) || !stride_wide(a->dv_row_stride, a->dv_head_stride)))
+    return DILOCO_ERR_MISALIGNED;
+  return DILOCO_OK;
+}
+
+AttnArgs args_of(const diloco_attention_t *a, const void *q, const void *k, const void *v, const int32_t *cu) {
+  AttnArgs r = {};
+  r.q = static_cast<const __nv_bfloat16 *>(q), r.k = static_cast<const __nv_bfloat16 *>(k), r.v = static_cast<const __nv_bfloat16 *>(v);
+  r.cu = cu;
+  r.q_row = a->q_row_stride, r.q_head = a->q_head_stride, r.k_row = a->k_row_stride, r.k_head = a->k_head_stride;
+  r.v_row = a->v_row_stride, r.v_head = a->v_head_stride, r.o_row = a->o_row_stride, r.o_head = a->o_head_stride;
+  r.do_row = a->do_row_stride, r.do_head = a->do_head_stride, r.dq_row = a->dq_row_stride, r.dq_head = a->dq_head_stride;
+  r.dk_row = a->dk_row_stride, r.dk_head = a->dk_head_stride, r.dv_row = a->dv_row_stride, r.dv_head = a->dv_head_stride;
+  r.tokens = (int)a->tokens, r.sequences = a->sequences, r.heads = a->heads, r.kv_heads = a->kv_heads;
+  r.group = a->heads / a->kv_heads, r.head_dim = a->head_dim;
+  r.scale = a->scale, r.scale_log2 = a->scale * kLog2e, r.status = a->device_status;
+  return r;
+}
+
+} // namespace
+} // namespace diloco
+
+using namespace diloco;
+
+extern "C" {
+
+int diloco_attention_forward(const diloco_attention_t *d, const void *q, const void *k, const void *v, const int32_t *cu_seqlens,
+                             void *out, float *lse, void *stream) {
+  const int rc = valid(d, false);
+  if (rc != DILOCO_OK) return rc;
+  if (d->tokens == 0) return DILOCO_OK;
+  PointerCheck pc;
+  pc.need(q, 16).need(k, 16).need(v, 16).need(cu_seqlens, 4).need(out, 16).need(lse, 4).maybe(d->device_status, 4);
+  if (pc.rc != DILOCO_OK) return pc.rc;
+  AttnArgs a = args_of(d, q, k, v, cu_seqlens);
+  a.out = static_cast<__nv_bfloat16 *>(out), a.lse = lse;
+  attn_forward_rows_kernel<<<dim3((a.tokens + kRowWarps - 1) / kRowWarps, a.heads), 32 * kRowWarps, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  return launched();
+}
+
+int64_t diloco_attention_workspace_bytes(const diloco_attention_t *d) {
+  const int rc = valid(d, true);
+  return rc != DILOCO_OK ? rc : d->tokens * d->heads * (int64_t)sizeof(float);
+}
+
+int diloco_attention_backward(const diloco_attention_t *d, const void *dout, const void *q, const void *k, const void *v,
+                              const void *out, const float *lse, const int32_t *cu_seqlens, void *dq, void *dk, void *dv,
+                              void *workspace, int64_t workspace_bytes, void *stream) {
+  int rc = valid(d, true);
+  if (rc != DILOCO_OK) return rc;
+  if (d->tokens == 0) return DILOCO_OK;
+  PointerCheck pc;
+  pc.need(dout, 16).need(q, 16).need(k, 16).need(v, 16).need(out, 16).need(lse, 4).need(cu_seqlens, 4);
+  pc.need(dq, 16).need(dk, 16).need(dv, 16).need(workspace, 256).maybe(d->device_status, 4);
+  if (pc.rc != DILOCO_OK) return pc.rc;
+  if (workspace_bytes < diloco_attention_workspace_bytes(d)) return DILOCO_ERR_INVALID_ARG;
+  AttnArgs a = args_of(d, q, k, v, cu_seqlens);
+  a.dout = static_cast<const __nv_bfloat16 *>(dout), a.out_in = static_cast<const __nv_bfloat16 *>(out);
+  a.lse = const_cast<float *>(lse), a.delta = static_cast<float *>(workspace);
+  a.dq = static_cast<__nv_bfloat16 *>(dq), a.dk = static_cast<__nv_bfloat16 *>(dk), a.dv = static_cast<__nv_bfloat16 *>(dv);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int blocks = (a.tokens + kRowWarps - 1) / kRowWarps;
+  attn_dq_rows_kernel<<<dim3(blocks, a.heads), 32 * kRowWarps, 0, s>>>(a);
+  rc = launched();
+  if (rc != DILOCO_OK) return rc;
+  attn_dkv_rows_kernel<<<dim3(blocks, a.kv_heads), 32 * kRowWarps, 0, s>>>(a);
+  return launched();
+}
+
+} // extern "C"

@@ -1,0 +1,522 @@
+// Scaled embedding lookup and its gradient by sorted tokens, for M replicas in one launch each.
+//
+// Forward: out[m, t] = scale * table[m, ids[m, t]], a gather of rows: memory alone bounds it.
+//
+// Backward: dtable[m, v] = scale * sum_{t: ids[m, t] = v} dout[m, t].  The bytes it cannot do without are
+// dout once and, unless it accumulates, the whole of dtable once (most rows zero: a text uses a part of the
+// vocabulary), so the tokens are put in order first and every row of dtable is then written once, by whoever
+// holds its sum, with no atomics on values.  Four launches, each one's start overlapping the end of the last:
+//   1 tiles    2048 tokens a block: stable partition by the id's low 8 bits (text uses low ids most, so low
+//              bits spread them: the top token of a 1/rank law is 7 % of the tokens, not half of a bucket)
+//   2 buckets  a block for each of the 256: gathers its pieces of all tiles in tile order, counts its ids, and
+//              places its tokens stably by id (every id belongs to one warp, which reads in order)
+//   3 sums     the sorted tokens in chunks of C, whatever ids they hold (an even split for any distribution): rows
+//              are added in order in registers; a run of one id inside a chunk is finished and written, a run
+//              that crosses chunks leaves fp32 partial sums.  The same launch zeroes the rows of absent ids.
+//   4 join     runs that cross chunks: partial sums in chunk order, written by the chunk where the run starts
+// Sums run in token order inside a chunk, then in chunk order: a fixed order for given ids.
+#include <type_traits>
+
+#include "diloco_ops.cuh"
+
+namespace diloco {
+namespace {
+
+constexpr int kTile = 2048, kTileThreads = 256, kBuckets = 256, kBucketBits = 8;
+constexpr int kMaxVocab = 1 << 20;
+constexpr int kMaxIds = kMaxVocab / kBuckets; // ids of one bucket
+constexpr int kWorkThreads = 256;
+
+struct EmbedArgs {
+  const void *ids, *table, *dout;
+  void *out, *dtable;
+  long long tokens, vocab, table_stride, grad_stride, row_stride;
+  int M, d, ids64, accumulate;
+  float scale;
+  // workspace of the backward, all [M, ...]
+  uint2 *tile_sorted, *gathered, *sorted; // [tokens] {id, token}: tile by tile, bucket by bucket, in order
+  unsigned *tile_off;          // [tiles, kBuckets + 1] first place of each bucket in a tile; last: its valid tokens
+  unsigned *count, *start;     // [vocab] tokens of an id, their first place in `sorted`
+  unsigned *total;             // [1] valid tokens
+  float *part;                 // [chunks, 2, d] run that began before the chunk, run that goes on after it
+  int tiles, chunks, C;
+};
+
+__device__ __forceinline__ long long id_at(const EmbedArgs &a, long long i) {
+  return a.ids64 ? static_cast<const long long *>(a.ids)[i] : (long long)static_cast<const int *>(a.ids)[i];
+}
+
+// ---------------------------------------------------------------------------------- forward
+template <typename TT, typename AT, int VW, int ROWS>
+__global__ void __launch_bounds__(kWorkThreads) embed_forward_kernel(const EmbedArgs a, int lanes) {
+  const int lane = threadIdx.x % lanes;
+  const long long n = a.tokens * a.M;
+  const long long r0 = ((long long)blockIdx.x * (kWorkThreads / lanes) + threadIdx.x / lanes) * ROWS;
+  long long src[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    src[i] = -1;
+    if (r0 + i < n) {
+      const long long id = id_at(a, r0 + i);
+      if (id >= 0 && id < a.vocab) src[i] = (r0 + i) / a.tokens * a.table_stride + id * a.d;
+    }
+  }
+  for (int col = lane * VW; col < a.d; col += lanes * VW) {
+    float v[ROWS][VW];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+      for (int j = 0; j < VW; ++j) v[i][j] = 0.f;
+      if (src[i] >= 0) load_wide<TT, VW>(static_cast<const TT *>(a.table) + src[i] + col, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+      if (r0 + i < n) {
+#pragma unroll
+        for (int j = 0; j < VW; ++j) v[i][j] *= a.scale;
+        store_wide<AT, VW>(static_cast<AT *>(a.out) + (r0 + i) * a.row_stride + col, v[i]);
+      }
+  }
+}
+
+// ---------------------------------------------------------------------------------- sorting
+__global__ void __launch_bounds__(kTileThreads) embed_tiles_kernel(const EmbedArgs a) {
+  constexpr int W = kTileThreads / 32, ROUNDS = kTile / kTileThreads;
+  __shared__ unsigned hist[W][kBuckets];
+  __shared__ unsigned warp_total[W];
+  const int m = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int w = 0; w < W; ++w) hist[w][threadIdx.x] = 0;
+  __syncthreads();
+  const long long first = (long long)blockIdx.x * kTile + warp * (kTile / W);
+  int id[ROUNDS], rank[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const long long t = first + r * 32 + lane;
+    long long v = t < a.tokens ? id_at(a, m * a.tokens + t) : -1;
+    id[r] = v >= 0 && v < a.vocab ? (int)v : -1;
+  }
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) { // a warp's tokens in order: ranks among equal buckets
+    const int b = id[r] < 0 ? kBuckets : id[r] & (kBuckets - 1);
+    const unsigned peers = __match_any_sync(0xffffffffu, b);
+    const int lead = __ffs(peers) - 1;
+    unsigned base = 0;
+    if (lane == lead && b < kBuckets) {
+      base = hist[warp][b];
+      hist[warp][b] = base + __popc(peers);
+    }
+    base = __shfl_sync(0xffffffffu, base, lead);
+    rank[r] = base + __popc(peers & ((1u << lane) - 1));
+    __syncwarp();
+  }
+  __syncthreads();
+  // thread b: where bucket b starts in the tile, and within it each warp's tokens
+  const int b = threadIdx.x;
+  unsigned sum = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const unsigned c = hist[w][b];
+    hist[w][b] = sum;
+    sum += c;
+  }
+  unsigned inc = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned up = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += up;
+  }
+  if (lane == 31) warp_total[warp] = inc;
+  __syncthreads();
+  unsigned before = inc - sum;
+  for (int w = 0; w < warp; ++w) before += warp_total[w];
+#pragma unroll
+  for (int w = 0; w < W; ++w) hist[w][b] += before;
+  unsigned *off = a.tile_off + ((long long)m * a.tiles + blockIdx.x) * (kBuckets + 1);
+  off[b] = before;
+  if (b == kBuckets - 1) off[kBuckets] = before + sum;
+  __syncthreads();
+  uint2 *out = a.tile_sorted + m * a.tokens + (long long)blockIdx.x * kTile;
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r)
+    if (id[r] >= 0)
+      out[hist[warp][id[r] & (kBuckets - 1)] + rank[r]] = make_uint2((unsigned)id[r], (unsigned)(first + r * 32 + lane));
+}
+
+// Sum of two values over the block's 256 threads.
+__device__ __forceinline__ uint2 block_sum(uint2 v, unsigned (*buf)[8]) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+  }
+  if ((threadIdx.x & 31) == 0) buf[0][threadIdx.x >> 5] = v.x, buf[1][threadIdx.x >> 5] = v.y;
+  __syncthreads();
+  v = make_uint2(0, 0);
+  for (int w = 0; w < 8; ++w) v.x += buf[0][w], v.y += buf[1][w];
+  __syncthreads();
+  return v;
+}
+
+// Inclusive sum over the block's 256 threads, in thread order; `all` is the whole sum.
+__device__ __forceinline__ unsigned block_scan(unsigned v, unsigned *buf, unsigned &all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned up = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += up;
+  }
+  if (lane == 31) buf[warp] = v;
+  __syncthreads();
+  all = 0;
+  for (int w = 0; w < 8; ++w) {
+    if (w < warp) v += buf[w];
+    all += buf[w];
+  }
+  __syncthreads();
+  return v;
+}
+
+__global__ void __launch_bounds__(256) embed_buckets_kernel(const EmbedArgs a) {
+  __shared__ unsigned cnt[kMaxIds]; // tokens of each id, then the next free place of each
+  __shared__ unsigned buf[2][8], scan[256], src[256];
+  const int m = blockIdx.y, b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int ids = b < a.vocab ? (int)((a.vocab - b + kBuckets - 1) >> kBucketBits) : 0; // b, b + 256, ... below vocab
+  for (int i = tid; i < ids; i += 256) cnt[i] = 0;
+  grid_wait();
+  const unsigned *off = a.tile_off + (long long)m * a.tiles * (kBuckets + 1) + b;
+  // a tile's offset of bucket b is its number of tokens in lower buckets
+  uint2 s = make_uint2(0, 0);
+  for (int t = tid; t < a.tiles; t += 256) {
+    const unsigned o = off[(long long)t * (kBuckets + 1)];
+    s.x += o;
+    s.y += off[(long long)t * (kBuckets + 1) + 1] - o;
+  }
+  s = block_sum(s, buf);
+  const unsigned base = s.x, n = s.y;
+  uint2 *gathered = a.gathered + m * a.tokens + base, *sorted = a.sorted + m * a.tokens + base;
+  const uint2 *tiles = a.tile_sorted + m * a.tokens;
+  // the bucket's pieces one after another, 256 tiles at a time, and the count of every id
+  unsigned done = 0, here;
+  for (int t0 = 0; t0 < a.tiles; t0 += 256, done += here) {
+    const int t = t0 + tid;
+    unsigned o = 0, c = 0;
+    if (t < a.tiles) {
+      o = off[(long long)t * (kBuckets + 1)];
+      c = off[(long long)t * (kBuckets + 1) + 1] - o;
+    }
+    scan[tid] = block_scan(c, buf[0], here) - c;
+    src[tid] = o;
+    __syncthreads();
+    for (unsigned e = tid; e < here; e += 256) {
+      int lo = 0, hi = 255; // the last tile that starts at or before entry e
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (scan[mid] <= e) lo = mid;
+        else hi = mid - 1;
+      }
+      const uint2 v = tiles[(long long)(t0 + lo) * kTile + src[lo] + (e - scan[lo])];
+      atomicAdd(&cnt[v.x >> kBucketBits], 1u);
+      gathered[done + e] = v;
+    }
+    __syncthreads();
+  }
+  unsigned run = 0;
+  for (int i0 = 0; i0 < ids; i0 += 256) {
+    const unsigned c = i0 + tid < ids ? cnt[i0 + tid] : 0;
+    unsigned all;
+    const unsigned at = run + block_scan(c, buf[0], all) - c;
+    run += all;
+    if (i0 + tid < ids) {
+      const long long v = m * a.vocab + b + (long long)(i0 + tid) * kBuckets;
+      a.count[v] = c;
+      a.start[v] = base + at;
+      cnt[i0 + tid] = at;
+    }
+  }
+  if (b == kBuckets - 1 && tid == 0) a.total[m] = base + n;
+  __syncthreads();
+  // stable placement: a warp walks the whole bucket in order and places the ids that are its own
+  for (unsigned e0 = 0; e0 < n; e0 += 128) {
+    uint2 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const unsigned e = e0 + k * 32 + lane;
+      v[k] = e < n ? gathered[e] : make_uint2(0xffffffffu, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const unsigned hi = v[k].x >> kBucketBits;
+      const bool mine = v[k].x != 0xffffffffu && (hi & 7) == (unsigned)warp;
+      const unsigned who = __ballot_sync(0xffffffffu, mine);
+      if (who == 0) continue;
+      if (mine) {
+        const unsigned peers = __match_any_sync(who, hi);
+        const int lead = __ffs(peers) - 1;
+        unsigned at = 0;
+        if (lane == lead) {
+          at = cnt[hi];
+          cnt[hi] = at + __popc(peers);
+        }
+        at = __shfl_sync(peers, at, lead);
+        sorted[at + __popc(peers & ((1u << lane) - 1))] = v[k];
+      }
+      __syncwarp();
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------- sums
+template <typename GT, int VW> __device__ __forceinline__ void put_row(const EmbedArgs &a, int m, unsigned id, int col, float (&acc)[VW]) {
+  GT *p = static_cast<GT *>(a.dtable) + m * a.grad_stride + (long long)id * a.d + col;
+#pragma unroll
+  for (int j = 0; j < VW; ++j) acc[j] *= a.scale;
+  if (a.accumulate) {
+    float old[VW];
+    load_wide<GT, VW>(p, old);
+#pragma unroll
+    for (int j = 0; j < VW; ++j) acc[j] += old[j];
+  }
+  store_wide<GT, VW>(p, acc);
+}
+
+// Blocks [0, sum_blocks): chunks, `lanes` threads each and VW columns a thread (blockIdx.z: further columns).
+// The other blocks zero the rows of ids that no token has.
+template <typename AT, typename GT, int VW>
+__global__ void __launch_bounds__(kWorkThreads) embed_sums_kernel(const EmbedArgs a, int lanes, int sum_blocks) {
+  const int m = blockIdx.y, lane = threadIdx.x % lanes, worker = threadIdx.x / lanes, workers = kWorkThreads / lanes;
+  const int col = (blockIdx.z * lanes + lane) * VW;
+  grid_wait();
+  if ((int)blockIdx.x >= sum_blocks) {
+    if (col >= a.d) return;
+    float zero[VW];
+#pragma unroll
+    for (int j = 0; j < VW; ++j) zero[j] = 0.f;
+    for (long long v = (long long)(blockIdx.x - sum_blocks) * workers + worker; v < a.vocab; v += (long long)(gridDim.x - sum_blocks) * workers)
+      if (a.count[m * a.vocab + v] == 0)
+        store_wide<GT, VW>(static_cast<GT *>(a.dtable) + m * a.grad_stride + v * a.d + col, zero);
+    return;
+  }
+  const unsigned total = a.total[m];
+  const uint2 *sorted = a.sorted + m * a.tokens;
+  const AT *dout = static_cast<const AT *>(a.dout) + m * a.tokens * a.row_stride + col;
+  const long long chunk = (long long)blockIdx.x * workers + worker;
+  const unsigned c0 = chunk < a.chunks ? (unsigned)(chunk * a.C) : total;
+  if (c0 >= total || col >= a.d) return; // whole workers leave, or lanes beyond the row: no warp-wide step follows
+  const unsigned c1 = min(c0 + a.C, total);
+  bool began = c0 > 0 && sorted[c0 - 1].x == sorted[c0].x;
+  float acc[VW];
+#pragma unroll
+  for (int j = 0; j < VW; ++j) acc[j] = 0.f;
+  float *part = a.part + ((long long)m * a.chunks + chunk) * 2 * a.d + col;
+  unsigned cur = sorted[c0].x;
+  for (unsigned e0 = c0; e0 < c1; e0 += 8) {
+    uint2 en[8];
+    float v[8][VW];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) en[k] = e0 + k < c1 ? sorted[e0 + k] : make_uint2(cur, 0xffffffffu);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+#pragma unroll
+      for (int j = 0; j < VW; ++j) v[k][j] = 0.f;
+      if (e0 + k < c1) load_wide<AT, VW>(dout + (long long)en[k].y * a.row_stride, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (e0 + k < c1) {
+        if (en[k].x != cur) { // the same for every thread of the worker
+          if (began) store_wide<float, VW>(part, acc);
+          else put_row<GT, VW>(a, m, cur, col, acc);
+          began = false;
+          cur = en[k].x;
+#pragma unroll
+          for (int j = 0; j < VW; ++j) acc[j] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < VW; ++j) acc[j] += v[k][j];
+      }
+    }
+  }
+  if (began) store_wide<float, VW>(part, acc);
+  else if (c1 < total && sorted[c1].x == cur) store_wide<float, VW>(part + a.d, acc);
+  else put_row<GT, VW>(a, m, cur, col, acc);
+}
+
+template <typename GT, int VW>
+__global__ void __launch_bounds__(kWorkThreads) embed_join_kernel(const EmbedArgs a, int lanes) {
+  const int m = blockIdx.y, lane = threadIdx.x % lanes, worker = threadIdx.x / lanes, workers = kWorkThreads / lanes;
+  const int col = (blockIdx.z * lanes + lane) * VW;
+  grid_wait();
+  const long long chunk = (long long)blockIdx.x * workers + worker;
+  if (chunk >= a.chunks || col >= a.d) return;
+  const unsigned total = a.total[m];
+  const unsigned long long end = (unsigned long long)(chunk + 1) * a.C;
+  if (end >= total) return; // the last chunk's last run goes on nowhere
+  const unsigned id = a.sorted[m * a.tokens + end - 1].x;
+  const unsigned first = a.start[m * a.vocab + id], last = first + a.count[m * a.vocab + id] - 1;
+  if (first / a.C != chunk || last / a.C == chunk) return;
+  const float *part = a.part + (long long)m * a.chunks * 2 * a.d + col;
+  float acc[VW];
+  load_wide<float, VW>(part + (chunk * 2 + 1) * a.d, acc);
+  const long long to = last / a.C;
+#pragma unroll 4
+  for (long long c = chunk + 1; c <= to; ++c) {
+    float v[VW];
+    load_wide<float, VW>(part + c * 2 * a.d, v);
+#pragma unroll
+    for (int j = 0; j < VW; ++j) acc[j] += v[j];
+  }
+  put_row<GT, VW>(a, m, id, col, acc);
+}
+
+// ------------------------------------------------------------------------------------ host
+int valid(const diloco_embedding_t *e) {
+  if (!e) return DILOCO_ERR_INVALID_ARG;
+  if (e->M < 1 || e->d < 1 || e->tokens < 0 || e->vocab < 1 || e->row_stride < e->d) return DILOCO_ERR_INVALID_ARG;
+  if (e->ids_int64 != 0 && e->ids_int64 != 1) return DILOCO_ERR_INVALID_ARG;
+  if (!dtype_ok(e->table_dtype) || !dtype_ok(e->act_dtype) || !dtype_ok(e->grad_dtype)) return DILOCO_ERR_INVALID_ARG;
+  if (e->vocab > kMaxVocab || e->M > 65535 || e->d > (1 << 20)) return DILOCO_ERR_UNSUPPORTED;
+  if (e->tokens > INT32_MAX / e->M) return DILOCO_ERR_UNSUPPORTED;
+  if (e->M > 1 && e->table_stride < e->vocab * e->d) return DILOCO_ERR_INVALID_ARG;
+  return DILOCO_OK;
+}
+
+// Threads of one row: one 16-byte access each, whole warps, at most the block.
+int lanes_for(int d, int vw) {
+  int lanes = 32;
+  while (lanes < kWorkThreads && lanes * vw < d) lanes *= 2;
+  return lanes;
+}
+
+// Tokens of one chunk: 32, more where that would give each SM over 64 chunks (its partial rows would cost more
+// than the finer split brings).
+int chunk_for(const diloco_embedding_t *e) {
+  int c = 32;
+  while (c < 256 && e->tokens * e->M / c > 148 * 64) c *= 2;
+  return c;
+}
+
+struct Layout {
+  int64_t tile_sorted, gathered, sorted, tile_off, count, start, total, part, bytes;
+  int tiles, chunks, C;
+};
+Layout layout(const diloco_embedding_t *e) {
+  Layout l;
+  l.C = chunk_for(e);
+  l.tiles = (int)((e->tokens + kTile - 1) / kTile);
+  l.chunks = (int)((e->tokens + l.C - 1) / l.C);
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t r = at;
+    at += (bytes + 255) / 256 * 256;
+    return r;
+  };
+  l.tile_sorted = take(8 * e->M * e->tokens);
+  l.gathered = take(8 * e->M * e->tokens);
+  l.sorted = take(8 * e->M * e->tokens);
+  l.tile_off = take(4ll * e->M * l.tiles * (kBuckets + 1));
+  l.count = take(4 * e->M * e->vocab);
+  l.start = take(4 * e->M * e->vocab);
+  l.total = take(4 * e->M);
+  l.part = take(4ll * e->M * l.chunks * 2 * e->d);
+  l.bytes = at;
+  return l;
+}
+
+template <typename A, typename B, typename F> void with_width(bool wide, F f) {
+  if (wide) f(A{}, B{}, std::integral_constant<int, (sizeof(A) == 4 && sizeof(B) == 4) ? 4 : 8>{});
+  else f(A{}, B{}, std::integral_constant<int, 1>{});
+}
+template <typename F> void with_types(int32_t x, int32_t y, bool wide, F f) {
+  if (x == DILOCO_DTYPE_F32 && y == DILOCO_DTYPE_F32) with_width<float, float>(wide, f);
+  else if (x == DILOCO_DTYPE_F32) with_width<float, __nv_bfloat16>(wide, f);
+  else if (y == DILOCO_DTYPE_F32) with_width<__nv_bfloat16, float>(wide, f);
+  else with_width<__nv_bfloat16, __nv_bfloat16>(wide, f);
+}
+
+EmbedArgs args_of(const diloco_embedding_t *e) {
+  EmbedArgs a = {};
+  a.tokens = e->tokens, a.vocab = e->vocab, a.table_stride = e->table_stride, a.grad_stride = e->grad_stride;
+  a.row_stride = e->row_stride, a.M = e->M, a.d = e->d, a.ids64 = e->ids_int64, a.scale = e->scale;
+  return a;
+}
+
+} // namespace
+} // namespace diloco
+
+using namespace diloco;
+
+extern "C" {
+
+int diloco_embedding_forward(const diloco_embedding_t *e, const void *ids, const void *table, void *out, void *stream) {
+  const int rc = valid(e);
+  if (rc != DILOCO_OK) return rc;
+  if (e->tokens == 0) return DILOCO_OK;
+  PointerCheck pc;
+  pc.need(ids, e->ids_int64 ? 8 : 4).need(table, dtype_bytes(e->table_dtype)).need(out, dtype_bytes(e->act_dtype));
+  if (pc.rc != DILOCO_OK) return pc.rc;
+  EmbedArgs a = args_of(e);
+  a.ids = ids, a.table = table, a.out = out;
+  const bool wide = e->d % 8 == 0 && e->table_stride % 8 == 0 && e->row_stride % 8 == 0 && aligned_to(table, 16) && aligned_to(out, 16);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  with_types(e->table_dtype, e->act_dtype, wide, [&](auto t, auto o, auto w) {
+    constexpr int ROWS = 2;
+    const int lanes = lanes_for(e->d, w.value);
+    const int64_t workers = kWorkThreads / lanes, n = e->tokens * e->M;
+    const int64_t grid = (n + workers * ROWS - 1) / (workers * ROWS);
+    embed_forward_kernel<decltype(t), decltype(o), w.value, ROWS><<<(unsigned)grid, kWorkThreads, 0, st>>>(a, lanes);
+  });
+  return launched();
+}
+
+int64_t diloco_embedding_workspace_bytes(const diloco_embedding_t *e) {
+  const int rc = valid(e);
+  return rc != DILOCO_OK ? rc : layout(e).bytes;
+}
+
+int diloco_embedding_backward(const diloco_embedding_t *e, const void *ids, const void *dout, void *dtable, int32_t accumulate,
+                              void *workspace, int64_t workspace_bytes, void *stream) {
+  int rc = valid(e);
+  if (rc != DILOCO_OK) return rc;
+  if (e->M > 1 && e->grad_stride < e->vocab * e->d) return DILOCO_ERR_INVALID_ARG;
+  const Layout l = layout(e);
+  PointerCheck pc;
+  if (e->tokens) pc.need(ids, e->ids_int64 ? 8 : 4).need(dout, dtype_bytes(e->act_dtype));
+  pc.need(dtable, dtype_bytes(e->grad_dtype)).need(workspace, 256);
+  if (pc.rc != DILOCO_OK) return pc.rc;
+  if (workspace_bytes < l.bytes) return DILOCO_ERR_INVALID_ARG;
+  if (e->tokens == 0 && accumulate) return DILOCO_OK;
+  char *ws = static_cast<char *>(workspace);
+  EmbedArgs a = args_of(e);
+  a.ids = ids, a.dout = dout, a.dtable = dtable, a.accumulate = accumulate != 0;
+  a.tile_sorted = reinterpret_cast<uint2 *>(ws + l.tile_sorted), a.gathered = reinterpret_cast<uint2 *>(ws + l.gathered);
+  a.sorted = reinterpret_cast<uint2 *>(ws + l.sorted), a.tile_off = reinterpret_cast<unsigned *>(ws + l.tile_off);
+  a.count = reinterpret_cast<unsigned *>(ws + l.count), a.start = reinterpret_cast<unsigned *>(ws + l.start);
+  a.total = reinterpret_cast<unsigned *>(ws + l.total), a.part = reinterpret_cast<float *>(ws + l.part);
+  a.tiles = l.tiles, a.chunks = l.chunks, a.C = l.C;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (l.tiles) {
+    embed_tiles_kernel<<<dim3(l.tiles, e->M), kTileThreads, 0, st>>>(a);
+    rc = launched();
+    if (rc != DILOCO_OK) return rc;
+  }
+  rc = launch_chained(embed_buckets_kernel, dim3(kBuckets, e->M), dim3(256), 0, st, a);
+  if (rc != DILOCO_OK) return rc;
+  const bool wide = e->d % 8 == 0 && e->grad_stride % 8 == 0 && e->row_stride % 8 == 0 && aligned_to(dtable, 16) &&
+                    (e->tokens == 0 || aligned_to(dout, 16));
+  const int sms = sm_count(pc.device);
+  with_types(e->act_dtype, e->grad_dtype, wide, [&](auto t, auto g, auto w) {
+    const int lanes = lanes_for(e->d, w.value), workers = kWorkThreads / lanes;
+    const int slabs = (e->d + lanes * w.value - 1) / (lanes * w.value);
+    const int sums = (l.chunks + workers - 1) / workers;
+    const int64_t rows = (e->vocab + workers - 1) / workers, most = (int64_t)sms * 4;
+    const int zeros = a.accumulate ? 0 : (int)(rows < most ? rows : most);
+    if (sums + zeros == 0) return;
+    rc = launch_chained(embed_sums_kernel<decltype(t), decltype(g), w.value>, dim3(sums + zeros, e->M, slabs), dim3(kWorkThreads), 0, st, a,
+                        lanes, sums);
+    if (rc != DILOCO_OK || l.chunks < 2) return;
+    rc = launch_chained(embed_join_kernel<decltype(g), w.value>, dim3(sums, e->M, slabs), dim3(kWorkThreads), 0, st, a, lanes);
+  });
+  return rc;
+}
+
+} // extern "C"

@@ -1,0 +1,551 @@
+// Layer norm over the last axis, forward and backward, for M replicas in one launch.
+//
+//   mean = sum x / d, rstd = 1 / sqrt(sum (x - mean)^2 / d + eps), y = w (x - mean) rstd + b
+//   dx = rstd (w dy - c1 - xh c2), c1 = sum(w dy) / d, c2 = sum(w dy xh) / d, xh = (x - mean) rstd
+//   dw = sum over rows of dy xh, db = sum over rows of dy
+//
+// A pass reads every activation once and writes once (4 bytes of traffic per bf16 element forward, 6
+// backward, against some 10-20 instructions), so memory bounds it and the layout serves the loads: TPR
+// threads hold one vector of d elements in registers, 16 bytes per access and CH accesses per thread, the
+// parameters stay in registers (persistent blocks), and the next vector's loads are issued before this
+// one's sums.  The variance is the two-pass form on the register copy: no cancellation for any mean.
+// The weights' gradients are summed in registers over a block's vectors, once per block into the
+// workspace, and joined there in block order by a second small kernel: the same bits every time.
+#include "diloco_ops.cuh"
+
+namespace diloco {
+namespace {
+
+struct NormArgs {
+  const void *x, *dy, *w, *b;
+  void *y, *dx;
+  float *mean, *rstd;
+  float *part; // [M, gridDim.x, 2, d] sums of one block
+  long long x_row, x_group, y_row, y_group, dx_row, dx_group, param_stride;
+  int R; // vectors per replica: rows * groups
+  int groups, d;
+  float eps;
+  int param_bf16, want_params;
+};
+
+__device__ __forceinline__ float param_at(const void *p, int bf16, long long i) {
+  return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]) : static_cast<const float *>(p)[i];
+}
+
+// Sum of N values over the TPR threads of a vector.  TPR > 32: the block is one vector's threads; `buf`
+// alternates between two halves so that one barrier per call is enough.
+template <int TPR, int N> __device__ __forceinline__ void row_sum(float (&v)[N], float (*buf)[N]) {
+#pragma unroll
+  for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  if (TPR > 32) {
+    constexpr int W = TPR / 32;
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) buf[threadIdx.x >> 5][i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += buf[w][i];
+  }
+}
+
+template <int TPR> struct Block { static constexpr int kThreads = TPR <= 32 ? 256 : TPR; };
+
+template <typename T, int VW, int TPR, int CH>
+__global__ void __launch_bounds__(Block<TPR>::kThreads, 1) norm_forward_kernel(const NormArgs a) {
+  constexpr int NT = Block<TPR>::kThreads, RPB = NT / TPR; // vectors of one block at a time
+  using Raw = typename Pack<T, VW>::raw;
+  __shared__ float buf[4][TPR > 32 ? TPR / 32 : 1][1];
+  const int m = blockIdx.y, lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const T *x = static_cast<const T *>(a.x);
+  T *y = static_cast<T *>(a.y);
+  bool in[CH];
+  float w[CH][VW], b[CH][VW];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * TPR + lane) * VW;
+    in[c] = col < a.d;
+#pragma unroll
+    for (int j = 0; j < VW; ++j) {
+      w[c][j] = in[c] ? param_at(a.w, a.param_bf16, m * a.param_stride + col + j) : 0.f;
+      b[c][j] = in[c] && a.b ? param_at(a.b, a.param_bf16, m * a.param_stride + col + j) : 0.f;
+    }
+  }
+  const float inv_d = 1.f / (float)a.d;
+  auto where = [&](int r, long long row_stride, long long group_stride) {
+    const int row = r / a.groups, g = r - row * a.groups;
+    const long long mr = (long long)m * (a.R / a.groups) + row;
+    return mr * row_stride + g * group_stride + lane * VW;
+  };
+  Raw next[CH];
+  auto fetch = [&](int r) {
+    if (r < a.R) {
+      const T *p = x + where(r, a.x_row, a.x_group);
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (in[c]) next[c] = *reinterpret_cast<const Raw *>(p + c * TPR * VW);
+    }
+  };
+  const int step = gridDim.x * RPB;
+  int half = 0;
+  fetch(blockIdx.x * RPB + sub);
+  for (int r0 = blockIdx.x * RPB; r0 < a.R; r0 += step) { // the same trips for every thread of the block
+    const int r = r0 + sub;
+    float v[CH][VW], s[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      unpack(next[c], v[c]);
+#pragma unroll
+      for (int j = 0; j < VW; ++j) {
+        if (!in[c] || r >= a.R) v[c][j] = 0.f;
+        s[0] += v[c][j];
+      }
+    }
+    fetch(r + step);
+    row_sum<TPR>(s, buf[half]);
+    const float mean = s[0] * inv_d;
+    s[0] = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < VW; ++j) {
+        v[c][j] -= mean;
+        if (in[c]) s[0] = fmaf(v[c][j], v[c][j], s[0]);
+      }
+    row_sum<TPR>(s, buf[half + 1]);
+    half ^= 2;
+    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_d, a.eps));
+    if (r < a.R) {
+      T *p = y + where(r, a.y_row, a.y_group);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+#pragma unroll
+        for (int j = 0; j < VW; ++j) v[c][j] = fmaf(w[c][j], v[c][j] * rstd, b[c][j]);
+        if (in[c]) store_vec<T, VW>(p + c * TPR * VW, v[c]);
+      }
+      if (lane == 0) {
+        const long long at = (long long)m * a.R + r;
+        if (a.mean) a.mean[at] = mean;
+        if (a.rstd) a.rstd[at] = rstd;
+      }
+    }
+  }
+}
+
+template <typename T, int VW, int TPR, int CH>
+__global__ void __launch_bounds__(Block<TPR>::kThreads, 1) norm_backward_kernel(const NormArgs a) {
+  constexpr int NT = Block<TPR>::kThreads, RPB = NT / TPR;
+  using Raw = typename Pack<T, VW>::raw;
+  __shared__ float buf[2][TPR > 32 ? TPR / 32 : 1][2];
+  // the vectors of a block that a warp or less holds meet here: [2, d] sums, d <= TPR * VW * CH
+  __shared__ float join[RPB > 1 ? 2 * TPR * VW * CH : 1];
+  const int m = blockIdx.y, lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
+  T *dx = static_cast<T *>(a.dx);
+  bool in[CH];
+  float w[CH][VW], dw[CH][VW], db[CH][VW];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * TPR + lane) * VW;
+    in[c] = col < a.d;
+#pragma unroll
+    for (int j = 0; j < VW; ++j) {
+      w[c][j] = in[c] ? param_at(a.w, a.param_bf16, m * a.param_stride + col + j) : 0.f;
+      dw[c][j] = db[c][j] = 0.f;
+    }
+  }
+  const float inv_d = 1.f / (float)a.d;
+  auto where = [&](int r, long long row_stride, long long group_stride) {
+    const int row = r / a.groups, g = r - row * a.groups;
+    const long long mr = (long long)m * (a.R / a.groups) + row;
+    return mr * row_stride + g * group_stride + lane * VW;
+  };
+  Raw nx[CH], ny[CH];
+  float nmean = 0.f, nrstd = 0.f;
+  auto fetch = [&](int r) {
+    if (r < a.R) {
+      const T *p = x + where(r, a.x_row, a.x_group), *q = dy + where(r, a.y_row, a.y_group);
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (in[c]) {
+          nx[c] = *reinterpret_cast<const Raw *>(p + c * TPR * VW);
+          ny[c] = *reinterpret_cast<const Raw *>(q + c * TPR * VW);
+        }
+      nmean = a.mean[(long long)m * a.R + r];
+      nrstd = a.rstd[(long long)m * a.R + r];
+    }
+  };
+  const int step = gridDim.x * RPB;
+  int half = 0;
+  fetch(blockIdx.x * RPB + sub);
+  for (int r0 = blockIdx.x * RPB; r0 < a.R; r0 += step) {
+    const int r = r0 + sub;
+    float xh[CH][VW], g[CH][VW], s[2] = {0.f, 0.f};
+    const float mean = nmean, rstd = nrstd;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      unpack(nx[c], xh[c]);
+      unpack(ny[c], g[c]);
+#pragma unroll
+      for (int j = 0; j < VW; ++j) {
+        if (!in[c] || r >= a.R) {
+          xh[c][j] = g[c][j] = 0.f;
+        } else {
+          xh[c][j] = (xh[c][j] - mean) * rstd;
+          dw[c][j] = fmaf(g[c][j], xh[c][j], dw[c][j]);
+          db[c][j] += g[c][j];
+          g[c][j] *= w[c][j];
+          s[0] += g[c][j];
+          s[1] = fmaf(g[c][j], xh[c][j], s[1]);
+        }
+      }
+    }
+    fetch(r + step);
+    row_sum<TPR>(s, buf[half]);
+    half ^= 1;
+    const float c1 = s[0] * inv_d, c2 = s[1] * inv_d;
+    if (r < a.R) {
+      T *p = dx + where(r, a.dx_row, a.dx_group);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+#pragma unroll
+        for (int j = 0; j < VW; ++j) g[c][j] = rstd * (g[c][j] - c1 - xh[c][j] * c2);
+        if (in[c]) store_vec<T, VW>(p + c * TPR * VW, g[c]);
+      }
+    }
+  }
+  if (!a.want_params) return;
+  float *part = a.part + ((long long)m * gridDim.x + blockIdx.x) * 2 * a.d;
+  if (RPB > 1) {
+    for (int turn = 0; turn < RPB; ++turn) { // in the order of the vectors' places in the block
+      if (sub == turn)
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+          for (int j = 0; j < VW; ++j) {
+            const int col = (c * TPR + lane) * VW + j;
+            float *pw = &join[RPB > 1 ? col : 0], *pb = &join[RPB > 1 ? TPR * VW * CH + col : 0];
+            *pw = turn ? *pw + dw[c][j] : dw[c][j];
+            *pb = turn ? *pb + db[c][j] : db[c][j];
+          }
+      __syncthreads();
+    }
+    for (int i = threadIdx.x; i < a.d; i += NT) {
+      part[i] = join[RPB > 1 ? i : 0];
+      part[a.d + i] = join[RPB > 1 ? TPR * VW * CH + i : 0];
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (c * TPR + lane) * VW;
+      if (in[c]) {
+        store_wide<float, VW>(part + col, dw[c]);
+        store_wide<float, VW>(part + a.d + col, db[c]);
+      }
+    }
+  }
+}
+
+// Vectors that no register layout holds (longer than 8192 bf16 or 4096 fp32 elements, or longer than 4096
+// with rows that 16-byte accesses do not reach): one block per vector walks it from memory, three times
+// forward and twice backward, after the first time from L2.
+constexpr int kLoopThreads = 512;
+template <typename T> __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const NormArgs a) {
+  __shared__ float buf[4][kLoopThreads / 32][1];
+  const int m = blockIdx.y;
+  const float inv_d = 1.f / (float)a.d;
+  int half = 0;
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
+    const int row = r / a.groups, g = r - row * a.groups;
+    const long long mr = (long long)m * (a.R / a.groups) + row;
+    const T *x = static_cast<const T *>(a.x) + mr * a.x_row + g * a.x_group;
+    T *y = static_cast<T *>(a.y) + mr * a.y_row + g * a.y_group;
+    float s[1] = {0.f}, v[1];
+    for (int i = threadIdx.x; i < a.d; i += kLoopThreads) {
+      load_vec<T, 1>(x + i, v);
+      s[0] += v[0];
+    }
+    row_sum<kLoopThreads>(s, buf[half]);
+    const float mean = s[0] * inv_d;
+    s[0] = 0.f;
+    for (int i = threadIdx.x; i < a.d; i += kLoopThreads) {
+      load_vec<T, 1>(x + i, v);
+      s[0] = fmaf(v[0] - mean, v[0] - mean, s[0]);
+    }
+    row_sum<kLoopThreads>(s, buf[half + 1]);
+    half ^= 2;
+    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_d, a.eps));
+    for (int i = threadIdx.x; i < a.d; i += kLoopThreads) {
+      load_vec<T, 1>(x + i, v);
+      const float w = param_at(a.w, a.param_bf16, m * a.param_stride + i);
+      const float b = a.b ? param_at(a.b, a.param_bf16, m * a.param_stride + i) : 0.f;
+      v[0] = fmaf(w, (v[0] - mean) * rstd, b);
+      store_vec<T, 1>(y + i, v);
+    }
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[(long long)m * a.R + r] = mean;
+      if (a.rstd) a.rstd[(long long)m * a.R + r] = rstd;
+    }
+  }
+}
+
+template <typename T> __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const NormArgs a) {
+  __shared__ float buf[2][kLoopThreads / 32][2];
+  const int m = blockIdx.y;
+  const float inv_d = 1.f / (float)a.d;
+  float *part = a.part + ((long long)m * gridDim.x + blockIdx.x) * 2 * a.d; // column i: one thread's alone
+  if (a.want_params)
+    for (int i = threadIdx.x; i < a.d; i += kLoopThreads) part[i] = part[a.d + i] = 0.f;
+  int half = 0;
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
+    const int row = r / a.groups, g = r - row * a.groups;
+    const long long mr = (long long)m * (a.R / a.groups) + row;
+    const T *x = static_cast<const T *>(a.x) + mr * a.x_row + g * a.x_group;
+    const T *dy = static_cast<const T *>(a.dy) + mr * a.y_row + g * a.y_group;
+    T *dx = static_cast<T *>(a.dx) + mr * a.dx_row + g * a.dx_group;
+    const float mean = a.mean[(long long)m * a.R + r], rstd = a.rstd[(long long)m * a.R + r];
+    float s[2] = {0.f, 0.f}, v[1], h[1];
+    for (int i = threadIdx.x; i < a.d; i += kLoopThreads) {
+      load_vec<T, 1>(x + i, v);
+      load_vec<T, 1>(dy + i, h);
+      v[0] = (v[0] - mean) * rstd;
+      if (a.want_params) {
+        part[i] = fmaf(h[0], v[0], part[i]);
+        part[a.d + i] += h[0];
+      }
+      h[0] *= param_at(a.w, a.param_bf16, m * a.param_stride + i);
+      s[0] += h[0];
+      s[1] = fmaf(h[0], v[0], s[1]);
+    }
+    row_sum<kLoopThreads>(s, buf[half]);
+    half ^= 1;
+    const float c1 = s[0] * inv_d, c2 = s[1] * inv_d;
+    for (int i = threadIdx.x; i < a.d; i += kLoopThreads) {
+      load_vec<T, 1>(x + i, v);
+      load_vec<T, 1>(dy + i, h);
+      v[0] = (v[0] - mean) * rstd;
+      h[0] *= param_at(a.w, a.param_bf16, m * a.param_stride + i);
+      h[0] = rstd * (h[0] - c1 - v[0] * c2);
+      store_vec<T, 1>(dx + i, h);
+    }
+  }
+}
+
+// dweight, dbias [d] of every replica from the blocks' sums: 32 columns a block, the parts dealt to 16 rows of
+// threads and joined in row order.
+constexpr int kJoinRows = 16;
+__global__ void __launch_bounds__(32 * kJoinRows) norm_params_kernel(const float *part, int parts, int d, void *dw, void *db,
+                                                                     long long grad_stride, int grad_bf16, int accumulate) {
+  __shared__ float sums[kJoinRows][32];
+  grid_wait();
+  const int m = blockIdx.y, which = blockIdx.z;
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, col = blockIdx.x * 32 + tx;
+  void *out = which ? db : dw;
+  if (!out) return;
+  float s = 0.f;
+  if (col < d) {
+    const float *p = part + ((long long)m * parts * 2 + which) * d + col;
+#pragma unroll 8
+    for (int i = ty; i < parts; i += kJoinRows) s += p[(long long)i * 2 * d];
+  }
+  sums[ty][tx] = s;
+  __syncthreads();
+  if (ty == 0 && col < d) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinRows; ++i) s += sums[i][tx];
+    const long long at = m * grad_stride + col;
+    if (grad_bf16) {
+      __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out) + at;
+      *o = __float2bfloat16_rn(accumulate ? s + __bfloat162float(*o) : s);
+    } else {
+      float *o = static_cast<float *>(out) + at;
+      *o = accumulate ? s + *o : s;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------ host
+enum { SHAPE_LOOP = -1 };
+struct Shape { // one register layout: vector width, threads per vector, accesses per thread
+  int vw, tpr, ch;
+};
+
+// The smallest layout that holds d elements.  A vector of at most 2 accesses per lane stays in one warp (no
+// barriers); longer ones take whole blocks.  Odd sizes and rows take single elements, 256 threads each.
+Shape shape_for(int d, int width, bool wide) {
+  if (!wide) return d <= 1024 ? Shape{1, 256, 4} : d <= 4096 ? Shape{1, 256, 16} : Shape{0, SHAPE_LOOP, 0};
+  const int n = d / width;
+  if (n <= 8) return {width, 8, 1};
+  if (n <= 16) return {width, 16, 1};
+  if (n <= 32) return {width, 32, 1};
+  if (n <= 64) return {width, 32, 2};
+  if (n <= 128) return {width, 64, 2};
+  if (n <= 256) return {width, 128, 2};
+  if (n <= 512) return {width, 256, 2};
+  if (n <= 1024) return {width, 512, 2};
+  return {0, SHAPE_LOOP, 0};
+}
+
+template <typename T, typename F> bool with_shape(const Shape &s, F f) {
+  constexpr int W = 16 / (int)sizeof(T);
+  if (s.tpr == SHAPE_LOOP) return false;
+#define DILOCO_NORM_SHAPE(VW_, TPR_, CH_)                                \
+  if (s.vw == VW_ && s.tpr == TPR_ && s.ch == CH_) {                     \
+    f(norm_forward_kernel<T, VW_, TPR_, CH_>, norm_backward_kernel<T, VW_, TPR_, CH_>); \
+    return true;                                                         \
+  }
+  DILOCO_NORM_SHAPE(W, 8, 1)
+  DILOCO_NORM_SHAPE(W, 16, 1)
+  DILOCO_NORM_SHAPE(W, 32, 1)
+  DILOCO_NORM_SHAPE(W, 32, 2)
+  DILOCO_NORM_SHAPE(W, 64, 2)
+  DILOCO_NORM_SHAPE(W, 128, 2)
+  DILOCO_NORM_SHAPE(W, 256, 2)
+  DILOCO_NORM_SHAPE(W, 512, 2)
+  DILOCO_NORM_SHAPE(1, 256, 4)
+  DILOCO_NORM_SHAPE(1, 256, 16)
+#undef DILOCO_NORM_SHAPE
+  return false;
+}
+
+int valid(const diloco_layernorm_t *n, bool backward) {
+  if (!n) return DILOCO_ERR_INVALID_ARG;
+  if (n->M < 1 || n->d < 1 || n->groups < 1 || n->rows < 0) return DILOCO_ERR_INVALID_ARG;
+  if (!dtype_ok(n->act_dtype) || !dtype_ok(n->param_dtype)) return DILOCO_ERR_INVALID_ARG;
+  if (n->x_row_stride < 0 || n->x_group_stride < 0 || n->y_row_stride < 0 || n->y_group_stride < 0) return DILOCO_ERR_INVALID_ARG;
+  if (n->M > 1 && n->param_stride < n->d) return DILOCO_ERR_INVALID_ARG;
+  if (!(n->eps >= 0.f)) return DILOCO_ERR_INVALID_ARG;
+  if (backward) {
+    if (!dtype_ok(n->grad_dtype) || n->dx_row_stride < 0 || n->dx_group_stride < 0) return DILOCO_ERR_INVALID_ARG;
+  }
+  if (n->M > 65535 || n->d > 65536 || n->rows > INT32_MAX / n->groups) return DILOCO_ERR_UNSUPPORTED;
+  return DILOCO_OK;
+}
+
+// Blocks for each replica: what the SMs hold at once, fewer where each would get less than a few vectors.
+int blocks_for(int R, int M, int per_block, int per_sm, int sms, int least) {
+  const int64_t want = ((int64_t)R + (int64_t)per_block * least - 1) / ((int64_t)per_block * least);
+  const int64_t most = ((int64_t)sms * per_sm + M - 1) / M;
+  return (int)(want < 1 ? 1 : want < most ? want : most);
+}
+
+// The backward's blocks are what sizes its workspace, so they follow from the descriptor and the SM count alone.
+int backward_blocks(const diloco_layernorm_t *n, int sms, bool wide) {
+  const Shape s = shape_for(n->d, n->act_dtype == DILOCO_DTYPE_F32 ? 4 : 8, wide);
+  const int R = (int)(n->rows * n->groups);
+  if (s.tpr == SHAPE_LOOP) return blocks_for(R, n->M, 1, 2, sms, 1);
+  const int nt = s.tpr <= 32 ? 256 : s.tpr;
+  return blocks_for(R, n->M, nt / s.tpr, 1024 / nt < 1 ? 1 : 1024 / nt, sms, 4);
+}
+
+int current_sms(int *sms) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_fail(e);
+  *sms = sm_count(dev);
+  return DILOCO_OK;
+}
+
+bool multiple(long long a, long long b, int w) { return a % w == 0 && b % w == 0; }
+
+} // namespace
+} // namespace diloco
+
+using namespace diloco;
+
+extern "C" {
+
+int diloco_layernorm_forward(const diloco_layernorm_t *n, const void *x, const void *weight, const void *bias, void *y,
+                             float *mean, float *rstd, void *stream) {
+  const int rc = valid(n, false);
+  if (rc != DILOCO_OK) return rc;
+  const int R = (int)(n->rows * n->groups);
+  if (R == 0) return DILOCO_OK;
+  const int64_t ea = dtype_bytes(n->act_dtype), ep = dtype_bytes(n->param_dtype);
+  PointerCheck pc;
+  pc.need(x, ea).need(weight, ep).maybe(bias, ep).need(y, ea).maybe(mean, 4).maybe(rstd, 4);
+  if (pc.rc != DILOCO_OK) return pc.rc;
+  NormArgs a = {};
+  a.x = x, a.w = weight, a.b = bias, a.y = y, a.mean = mean, a.rstd = rstd;
+  a.x_row = n->x_row_stride, a.x_group = n->x_group_stride, a.y_row = n->y_row_stride, a.y_group = n->y_group_stride;
+  a.param_stride = n->param_stride, a.R = R, a.groups = n->groups, a.d = n->d, a.eps = n->eps;
+  a.param_bf16 = n->param_dtype == DILOCO_DTYPE_BF16;
+  const int width = (int)(16 / ea);
+  const bool wide = aligned_to(x, 16) && aligned_to(y, 16) && n->d % width == 0 && multiple(a.x_row, a.x_group, width) &&
+                    multiple(a.y_row, a.y_group, width);
+  const Shape s = shape_for(n->d, width, wide);
+  const int sms = sm_count(pc.device);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  auto go = [&](auto f, auto) {
+    const int nt = s.tpr <= 32 ? 256 : s.tpr;
+    const int g = blocks_for(R, n->M, nt / s.tpr, 2048 / nt, sms, 1);
+    f<<<dim3(g, n->M), nt, 0, st>>>(a);
+  };
+  if (n->act_dtype == DILOCO_DTYPE_F32) {
+    if (!with_shape<float>(s, go)) norm_forward_loop_kernel<float><<<dim3(blocks_for(R, n->M, 1, 4, sms, 1), n->M), kLoopThreads, 0, st>>>(a);
+  } else {
+    if (!with_shape<__nv_bfloat16>(s, go)) norm_forward_loop_kernel<__nv_bfloat16><<<dim3(blocks_for(R, n->M, 1, 4, sms, 1), n->M), kLoopThreads, 0, st>>>(a);
+  }
+  return launched();
+}
+
+int64_t diloco_layernorm_workspace_bytes(const diloco_layernorm_t *n) {
+  int rc = valid(n, true), sms = 0;
+  if (rc == DILOCO_OK) rc = current_sms(&sms);
+  if (rc != DILOCO_OK) return rc;
+  const int a = backward_blocks(n, sms, true), b = backward_blocks(n, sms, false);
+  return (int64_t)(a > b ? a : b) * n->M * 2 * n->d * (int64_t)sizeof(float);
+}
+
+int diloco_layernorm_backward(const diloco_layernorm_t *n, const void *dy, const void *x, const void *weight, const float *mean,
+                              const float *rstd, void *dx, void *dweight, void *dbias, int32_t accumulate, void *workspace,
+                              int64_t workspace_bytes, void *stream) {
+  int rc = valid(n, true);
+  if (rc != DILOCO_OK) return rc;
+  const int R = (int)(n->rows * n->groups);
+  const int64_t ea = dtype_bytes(n->act_dtype), ep = dtype_bytes(n->param_dtype), eg = dtype_bytes(n->grad_dtype);
+  const bool want = dweight || dbias;
+  if (want && n->M > 1 && n->grad_stride < n->d) return DILOCO_ERR_INVALID_ARG;
+  PointerCheck pc;
+  if (R) pc.need(dy, ea).need(x, ea).need(weight, ep).need(mean, 4).need(rstd, 4).need(dx, ea);
+  pc.maybe(dweight, eg).maybe(dbias, eg);
+  if (want) pc.need(workspace, 256);
+  if (pc.rc != DILOCO_OK) return pc.rc;
+  const int sms = sm_count(pc.device), width = (int)(16 / ea);
+  NormArgs a = {};
+  a.x = x, a.dy = dy, a.w = weight, a.dx = dx, a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
+  a.x_row = n->x_row_stride, a.x_group = n->x_group_stride, a.y_row = n->y_row_stride, a.y_group = n->y_group_stride;
+  a.dx_row = n->dx_row_stride, a.dx_group = n->dx_group_stride;
+  a.param_stride = n->param_stride, a.R = R, a.groups = n->groups, a.d = n->d, a.eps = n->eps;
+  a.param_bf16 = n->param_dtype == DILOCO_DTYPE_BF16, a.want_params = want, a.part = static_cast<float *>(workspace);
+  const bool wide = aligned_to(x, 16) && aligned_to(dy, 16) && aligned_to(dx, 16) && n->d % width == 0 &&
+                    multiple(a.x_row, a.x_group, width) && multiple(a.y_row, a.y_group, width) && multiple(a.dx_row, a.dx_group, width);
+  const Shape s = shape_for(n->d, width, wide);
+  const int g = backward_blocks(n, sms, wide);
+  if (want && workspace_bytes < (int64_t)g * n->M * 2 * n->d * (int64_t)sizeof(float)) return DILOCO_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int parts = 0;
+  if (R) {
+    auto go = [&](auto, auto f) { f<<<dim3(g, n->M), s.tpr <= 32 ? 256 : s.tpr, 0, st>>>(a); };
+    if (n->act_dtype == DILOCO_DTYPE_F32) {
+      if (!with_shape<float>(s, go)) norm_backward_loop_kernel<float><<<dim3(g, n->M), kLoopThreads, 0, st>>>(a);
+    } else {
+      if (!with_shape<__nv_bfloat16>(s, go)) norm_backward_loop_kernel<__nv_bfloat16><<<dim3(g, n->M), kLoopThreads, 0, st>>>(a);
+    }
+    rc = launched();
+    if (rc != DILOCO_OK) return rc;
+    parts = g;
+  }
+  if (!want) return DILOCO_OK;
+  return launch_chained(norm_params_kernel, dim3((n->d + 31) / 32, n->M, 2), dim3(32 * kJoinRows), 0, st,
+                        (const float *)workspace, parts, (int)n->d, dweight, dbias, (long long)n->grad_stride,
+                        (int)(n->grad_dtype == DILOCO_DTYPE_BF16), (int)accumulate);
+}
+
+} // extern "C"

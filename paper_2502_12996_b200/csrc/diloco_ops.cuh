@@ -1,0 +1,155 @@
+// What the decoder operators (embedding, layer norm, attention, distillation loss) share: argument
+// checks on the host, loads and stores of fp32 / bf16 elements and block sums on the device.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/diloco.h"
+
+namespace diloco {
+
+int cuda_fail(cudaError_t e);                             // records the error, returns DILOCO_ERR_CUDA
+void count_launch();                                      // one more kernel of this library
+int check_device_pointer(const void *p, int device);      // device or managed memory of `device`
+
+// ------------------------------------------------------------------------------------ host
+inline bool dtype_ok(int32_t t) { return t == DILOCO_DTYPE_F32 || t == DILOCO_DTYPE_BF16; }
+inline int64_t dtype_bytes(int32_t t) { return t == DILOCO_DTYPE_F32 ? 4 : 2; }
+inline bool aligned_to(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// The pointers of one call: every one is memory of the current device and aligned to `align`.
+struct PointerCheck {
+  int device = 0;
+  int rc = DILOCO_OK;
+  PointerCheck() {
+    const cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) rc = cuda_fail(e);
+  }
+  PointerCheck &need(const void *p, uintptr_t align) {
+    if (rc != DILOCO_OK) return *this;
+    if (!p) rc = DILOCO_ERR_INVALID_ARG;
+    else if (!aligned_to(p, align)) rc = DILOCO_ERR_MISALIGNED;
+    else rc = check_device_pointer(p, device);
+    return *this;
+  }
+  PointerCheck &maybe(const void *p, uintptr_t align) { return p ? need(p, align) : *this; }
+};
+
+inline int sm_count(int device) {
+  int n = 0;
+  return cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) == cudaSuccess && n > 0 ? n : 148;
+}
+
+inline int launched() {
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return cuda_fail(e);
+  count_launch();
+  return DILOCO_OK;
+}
+
+// Launch whose prologue may overlap the end of the kernel before it on the stream; the kernel calls
+// grid_wait() before it touches what an earlier kernel wrote or still reads.
+template <typename... KArgs, typename... Args>
+int launch_chained(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return cuda_fail(e);
+  }
+  count_launch();
+  return DILOCO_OK;
+}
+
+// ---------------------------------------------------------------------------------- device
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// 2^x by the special-function unit (2^-22 relative), 0 for x = -infinity and below the normal range
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// V consecutive elements as floats; one access of V * sizeof(T) bytes (at most 16).
+template <typename T, int V> struct Pack;
+template <> struct Pack<float, 1> { using raw = float; };
+template <> struct Pack<float, 2> { using raw = float2; };
+template <> struct Pack<float, 4> { using raw = float4; };
+template <> struct Pack<__nv_bfloat16, 1> { using raw = unsigned short; };
+template <> struct Pack<__nv_bfloat16, 2> { using raw = unsigned; };
+template <> struct Pack<__nv_bfloat16, 4> { using raw = uint2; };
+template <> struct Pack<__nv_bfloat16, 8> { using raw = uint4; };
+
+__device__ __forceinline__ float bf16_lo(unsigned w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ unsigned bf16_pair(float lo, float hi) { // round to nearest even, lo in bits 0-15
+  unsigned r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+__device__ __forceinline__ void unpack(const float &r, float (&v)[1]) { v[0] = r; }
+__device__ __forceinline__ void unpack(const float2 &r, float (&v)[2]) { v[0] = r.x, v[1] = r.y; }
+__device__ __forceinline__ void unpack(const float4 &r, float (&v)[4]) { v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w; }
+__device__ __forceinline__ void unpack(const unsigned short &r, float (&v)[1]) { v[0] = __uint_as_float((unsigned)r << 16); }
+__device__ __forceinline__ void unpack(const unsigned &r, float (&v)[2]) { v[0] = bf16_lo(r), v[1] = bf16_hi(r); }
+__device__ __forceinline__ void unpack(const uint2 &r, float (&v)[4]) {
+  v[0] = bf16_lo(r.x), v[1] = bf16_hi(r.x), v[2] = bf16_lo(r.y), v[3] = bf16_hi(r.y);
+}
+__device__ __forceinline__ void unpack(const uint4 &r, float (&v)[8]) {
+  v[0] = bf16_lo(r.x), v[1] = bf16_hi(r.x), v[2] = bf16_lo(r.y), v[3] = bf16_hi(r.y);
+  v[4] = bf16_lo(r.z), v[5] = bf16_hi(r.z), v[6] = bf16_lo(r.w), v[7] = bf16_hi(r.w);
+}
+__device__ __forceinline__ void pack(const float (&v)[1], float &r) { r = v[0]; }
+__device__ __forceinline__ void pack(const float (&v)[2], float2 &r) { r = make_float2(v[0], v[1]); }
+__device__ __forceinline__ void pack(const float (&v)[4], float4 &r) { r = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void pack(const float (&v)[1], unsigned short &r) { r = (unsigned short)bf16_pair(v[0], 0.f); }
+__device__ __forceinline__ void pack(const float (&v)[2], unsigned &r) { r = bf16_pair(v[0], v[1]); }
+__device__ __forceinline__ void pack(const float (&v)[4], uint2 &r) { r = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])); }
+__device__ __forceinline__ void pack(const float (&v)[8], uint4 &r) {
+  r = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+}
+
+template <typename T, int V> __device__ __forceinline__ void load_vec(const T *p, float (&v)[V]) {
+  unpack(*reinterpret_cast<const typename Pack<T, V>::raw *>(p), v);
+}
+// V values as 16-byte (or smaller) accesses, whatever V is
+template <typename T, int V> __device__ __forceinline__ void load_wide(const T *p, float (&v)[V]) {
+  constexpr int W = V * sizeof(T) <= 16 ? V : 16 / (int)sizeof(T);
+#pragma unroll
+  for (int i = 0; i < V; i += W) {
+    float t[W];
+    load_vec<T, W>(p + i, t);
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[i + j] = t[j];
+  }
+}
+template <typename T, int V> __device__ __forceinline__ void store_vec(T *p, const float (&v)[V]) {
+  typename Pack<T, V>::raw r;
+  pack(v, r);
+  *reinterpret_cast<typename Pack<T, V>::raw *>(p) = r;
+}
+template <typename T, int V> __device__ __forceinline__ void store_wide(T *p, const float (&v)[V]) {
+  constexpr int W = V * sizeof(T) <= 16 ? V : 16 / (int)sizeof(T);
+#pragma unroll
+  for (int i = 0; i < V; i += W) {
+    float t[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) t[j] = v[i + j];
+    store_vec<T, W>(p + i, t);
+  }
+}
+
+} // namespace diloco

@@ -13,6 +13,7 @@ namespace diloco {
 // defined next to the C ABI: record the failing cudaError_t / count a successful launch
 int cuda_fail(cudaError_t e);
 void count_launch();
+int check_device_pointer(const void *p, int device);
 
 // The one (variant, theta storage) -> template-argument ladder: f is called with two
 // std::integral_constant tags.

@@ -1,0 +1,706 @@
+"""The decoder operators on the GPU against their definitions in 64 bits, at the sizes, strides, masks and
+values where they can go wrong; their gradients also against differences.
+
+Tolerances, set before the first run from the arithmetic alone (u = 2^-24 for fp32, 2^-9 for a rounding to bf16):
+  fp32 results of sums over n terms   |got - want| <= 4 sqrt(n) u sum|terms|   (4 sigma of n random roundings, at least 16 u)
+  results stored as bf16              the fp32 bound plus half a bf16 ulp: 2^-8 of |want| (one rounding, bound doubled)
+  attention                           P and dz rounded to bf16 as operands: each output is a sum of terms off by 2^-9
+                                      relatively at most, so it is off by at most 2^-9 sum|terms|; bound doubled for the
+                                      fp32 part and the unnormalised accumulation, plus the storage rounding.  delta is taken
+                                      from the stored out: dz is off by up to 2^-9 P sum|dout||out| more (doubled as well)
+"""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2502_12996_b200 import binding, ops
+from gpu_util import guarded
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U32, UBF = 2.0 ** -24, 2.0 ** -9
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def _device():
+    torch.cuda.set_device(0)
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def randn(g, *shape, dtype=F32, std=1.0, mean=0.0):
+    return (torch.randn(shape, generator=g, device=DEV) * std + mean).to(dtype)
+
+
+def close(got, want, bound, what=""):
+    """|got - want| <= bound elementwise, plus the storage rounding of a bf16 result; same non-finite places."""
+    want = want.double()
+    g = got.double()
+    bound = bound + (want.abs() * 2.0 ** -8 if got.dtype == BF16 else 0.0)
+    odd = ~torch.isfinite(want)
+    assert torch.equal(torch.isnan(g), torch.isnan(want)), f"{what}: NaN in other places"
+    assert torch.equal(g[odd].nan_to_num(0.0), want[odd].nan_to_num(0.0)), f"{what}: non-finite values differ"
+    err = (g - want).abs()
+    bad = ~odd & (err > bound)
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst by {float((err - bound)[bad].max()):.3g} (error {float(err[bad].max()):.3g})"
+
+
+def sum_bound(n, terms):
+    """Bound of an fp32 sum of n terms whose absolute values sum to `terms`."""
+    return max(16.0, 4.0 * math.sqrt(n)) * U32 * terms + 1e-30
+
+
+# ------------------------------------------------------------------------------------ embedding
+def embed_want(ids, table, scale):
+    M, T = ids.shape
+    V = table.shape[1]
+    ok = (ids >= 0) & (ids < V)
+    rows = torch.stack([table[m].double()[ids[m].long().clamp(0, V - 1)] for m in range(M)]) if T else table.new_zeros((M, 0, table.shape[2])).double()
+    return rows * scale * ok[..., None]
+
+
+def embed_grad_want(ids, dout, V, scale):
+    M, T, d = dout.shape
+    want, size = (torch.zeros((M, V + 1, d), dtype=torch.float64, device=DEV) for _ in range(2))
+    at = torch.where((ids >= 0) & (ids < V), ids.long(), torch.full_like(ids.long(), V))
+    for m in range(M):
+        want[m].index_add_(0, at[m], dout[m].double())
+        size[m].index_add_(0, at[m], dout[m].double().abs())
+    return want[:, :V] * scale, size[:, :V] * abs(scale)
+
+
+EMBED = [  # M, tokens, vocab, d, table dtype, activations, gradients, ids
+    (1, 1, 1, 1, F32, F32, F32, torch.int32),
+    (1, 17, 100, 512, F32, F32, F32, torch.int32),
+    (2, 33, 7, 24, BF16, BF16, F32, torch.int64),           # every id many times
+    (3, 1000, 300, 100, BF16, F32, BF16, torch.int32),      # rows of 200 bytes
+    (2, 2049, 32000, 64, F32, BF16, F32, torch.int64),      # one token over a tile
+    (1, 5000, 1, 40, BF16, BF16, F32, torch.int32),         # one id for all: its run crosses every chunk
+    (4, 4096, 257, 37, F32, F32, BF16, torch.int32),        # odd width: single elements
+    (1, 70001, 50021, 72, BF16, BF16, BF16, torch.int32),
+    (2, 40000, 3, 2056, BF16, BF16, F32, torch.int32),      # wider than a block's one step
+    (1, 600000, 4100, 8, F32, F32, F32, torch.int32),       # over 256 tiles, longer chunks
+]
+
+
+@pytest.mark.parametrize("M,T,V,d,tdt,adt,gdt,idt", EMBED)
+def test_embedding(M, T, V, d, tdt, adt, gdt, idt):
+    g = gen(T + V)
+    u = torch.rand((M, T), generator=g, device=DEV, dtype=torch.float64)
+    ids = (torch.exp(u * math.log(V + 1.0)) - 1.0).to(idt).clamp_(0, V - 1)
+    if T > 16:
+        ids[:, 5], ids[:, 9], ids[0, 11] = -1, V, -2 ** 31     # no token
+    scale = math.sqrt(d)
+    pad = 64
+    flat = randn(g, M, V * d + pad, dtype=tdt)                 # the replicas' flat vectors
+    table = flat[:, :V * d].view(M, V, d) if M > 1 else flat[:, :V * d].reshape(M, V, d)
+    out, check = guarded((M, T, d), adt, DEV)
+    ops.embedding_forward(ids, table, scale=scale, out=out)
+    check()
+    want = embed_want(ids, table, scale)
+    close(out, want, 4 * U32 * want.abs(), "out")
+
+    dout = randn(g, M, T, d, dtype=adt)
+    want, size = embed_grad_want(ids, dout, V, scale)
+    bound = sum_bound(T, size)
+    grads, check = guarded((M, V * d + pad), gdt, DEV, fill=torch.full((M, V * d + pad), 3.0))
+    dtable = grads[:, :V * d].view(M, V, d) if M > 1 else grads[:, :V * d].reshape(M, V, d)
+    assert dtable.data_ptr() == grads.data_ptr()
+    before = binding.launch_count()
+    ops.embedding_backward(ids, dout, dtable, scale=scale)
+    assert binding.launch_count() > before
+    first = dtable.clone()
+    close(dtable, want, bound, "dtable")
+    ops.embedding_backward(ids, dout, dtable, scale=scale)
+    assert torch.equal(dtable, first), "the same call twice"
+    # accumulate: rows of absent ids keep their bits
+    old = randn(g, M, V, d, dtype=gdt)
+    dtable.copy_(old)
+    ops.embedding_backward(ids, dout, dtable, scale=scale, accumulate=True)
+    close(dtable, want + old.double(), bound + 4 * U32 * old.double().abs(), "accumulated")
+    absent = size.sum(-1) == 0
+    assert torch.equal(dtable[absent], old[absent])
+    assert bool((grads[:, V * d:] == 3.0).all()), "the next parameters of the flat gradient"
+    check()
+
+
+def test_embedding_without_tokens():
+    ids = torch.zeros((2, 0), dtype=torch.int32, device=DEV)
+    table = randn(gen(1), 2, 10, 16)
+    assert ops.embedding_forward(ids, table).shape == (2, 0, 16)
+    dtable = torch.ones_like(table)
+    ops.embedding_backward(ids, table.new_zeros((2, 0, 16)), dtable, accumulate=True)
+    assert bool((dtable == 1).all())
+    ops.embedding_backward(ids, table.new_zeros((2, 0, 16)), dtable)
+    assert bool((dtable == 0).all())
+    ids = torch.full((1, 100), -1, dtype=torch.int32, device=DEV)   # nothing but places without a token
+    dtable = torch.ones((1, 10, 16), device=DEV)
+    ops.embedding_backward(ids, torch.full((1, 100, 16), math.nan, device=DEV), dtable)
+    assert bool((dtable == 0).all())
+    assert bool((ops.embedding_forward(ids, table[:1]) == 0).all())
+
+
+def test_embedding_strided_rows_and_nonfinite():
+    """Rows inside wider rows; an infinite gradient reaches its own token's row only."""
+    g = gen(3)
+    wide = randn(g, 1, 300, 96)
+    dout = wide[:, :, :64]
+    dout[0, 7] = math.inf
+    ids = torch.randint(0, 50, (1, 300), generator=g, device=DEV, dtype=torch.int32)
+    dtable = torch.empty((1, 50, 64), device=DEV)
+    ops.embedding_backward(ids, dout, dtable)
+    rows = torch.isinf(dtable).any(-1)[0].nonzero().flatten().tolist()
+    assert rows == [int(ids[0, 7])]
+
+
+# ----------------------------------------------------------------------------------- layer norm
+NORM = [  # M, rows, groups, d, activations, parameters, gradients
+    (1, 1, 1, 1, F32, F32, F32),
+    (1, 48, 1, 512, BF16, F32, F32),
+    (2, 37, 1, 64, BF16, BF16, BF16),
+    (3, 29, 5, 128, BF16, BF16, F32),
+    (1, 300, 8, 80, F32, F32, F32),
+    (2, 65, 1, 1001, F32, F32, F32),
+    (1, 33, 1, 1001, BF16, F32, F32),
+    (2, 700, 1, 2048, BF16, F32, F32),
+    (1, 64, 1, 1024, F32, BF16, F32),
+    (1, 9, 1, 3000, BF16, F32, BF16),
+    (1, 33, 1, 4096, F32, F32, F32),
+    (1, 21, 1, 8192, BF16, F32, F32),
+    (1, 5, 1, 4099, F32, F32, F32),          # no register layout: odd and long
+    (1, 5, 1, 20000, BF16, F32, F32),
+]
+
+
+def norm_want(x, w, b, eps):
+    x = x.double()
+    shape = [w.shape[0]] + [1] * (x.dim() - 2) + [w.shape[1]]
+    w = w.double().view(shape)
+    b = torch.zeros_like(w) if b is None else b.double().view(shape)
+    mean = x.mean(-1, keepdim=True)
+    rstd = 1.0 / torch.sqrt(((x - mean) ** 2).mean(-1, keepdim=True) + eps)
+    xh = (x - mean) * rstd
+    return xh * w + b, mean, rstd, xh, w
+
+
+@pytest.mark.parametrize("bias", [True, False])
+@pytest.mark.parametrize("M,N,G,d,adt,pdt,gdt", NORM)
+def test_layer_norm(M, N, G, d, adt, pdt, gdt, bias):
+    g = gen(N * d)
+    eps = 1e-5
+    shape = (M, N, G, d) if G > 1 else (M, N, d)
+    if G > 1:
+        x = randn(g, M, N, 3 * G, d, std=2.0, mean=0.5).to(adt)[:, :, G:2 * G]       # the middle projection of a fused row
+    else:
+        x = randn(g, *shape, std=2.0, mean=30.0).to(adt)                             # a mean far above the deviation
+    w, b = randn(g, M, d + 3, std=0.3, mean=1.0, dtype=pdt)[:, :d], randn(g, M, d + 3, dtype=pdt)[:, :d] if bias else None
+    if M == 1:
+        w, b = w.reshape(1, d), b.reshape(1, d) if bias else None
+    out, check = guarded(shape, adt, DEV)
+    y, mean, rstd = ops.layer_norm_forward(x, w, b, eps=eps, out=out)
+    check()
+    want, mw, rw, xh, wd = norm_want(x, w, b, eps)
+    size = x.double().abs().mean(-1, keepdim=True)
+    me = sum_bound(d, size)                                        # of the mean
+    dev = (x.double() - mw).abs()
+    # rstd: relative error of a sum of squares, whose terms carry the mean's error to second order only
+    re = (max(16.0, 4.0 * math.sqrt(d)) * U32 + (me * rw) ** 2)
+    close(mean, mw.squeeze(-1), me.squeeze(-1), "mean")
+    close(rstd, rw.squeeze(-1), (re * rw).squeeze(-1), "rstd")
+    xe = (me + 4 * U32 * (dev + mw.abs())) * rw + re * xh.abs()    # of xh
+    close(y, want, xe * wd.abs() + 8 * U32 * (want.abs() + (xh * wd).abs()), "y")
+
+    dy = randn(g, *shape, dtype=adt)
+    n = N * G
+    dxh = dy.double() * wd
+    c1, c2 = dxh.mean(-1, keepdim=True), (dxh * xh).mean(-1, keepdim=True)
+    dxw = rw * (dxh - c1 - xh * c2)
+    s1, s2 = dxh.abs().mean(-1, keepdim=True), (dxh * xh).abs().mean(-1, keepdim=True)
+    c2e = sum_bound(d, s2) + (dxh.abs() * xe).mean(-1, keepdim=True)
+    bound = rw * (8 * U32 * (dxh.abs() + c1.abs() + (xh * c2).abs()) + sum_bound(d, s1) + xh.abs() * c2e + xe * c2.abs()) + 2 * re * dxw.abs()
+    flat = lambda t: t.reshape(M, -1, d)  # noqa: E731
+    dww, dws = flat(dy.double() * xh).sum(1), flat((dy.double() * xh).abs()).sum(1)
+    dwe = sum_bound(n, dws) + flat(dy.double().abs() * xe).sum(1)
+    dbw, dbs = flat(dy.double()).sum(1), flat(dy.double().abs()).sum(1)
+    grads = torch.full((2, M, d + 5), 7.0, device=DEV, dtype=gdt)
+    dw, db = grads[0, :, :d], grads[1, :, :d] if bias else None
+    dx, check = guarded(shape, adt, DEV)
+    ops.layer_norm_backward(dy, x, w, mean, rstd, dw, db, dx=dx)
+    check()
+    close(dx, dxw, bound, "dx")
+    close(dw, dww, dwe, "dweight")
+    assert bool((grads[:, :, d:] == 7.0).all())
+    first = dx.clone(), grads.clone()
+    ops.layer_norm_backward(dy, x, w, mean, rstd, dw, db, dx=dx)
+    assert torch.equal(first[0], dx) and torch.equal(first[1], grads), "the same call twice"
+    if bias:
+        close(db, dbw, sum_bound(n, dbs), "dbias")
+        old = dw.double().clone()
+        ops.layer_norm_backward(dy, x, w, mean, rstd, dw, db, dx=dx, accumulate=True)
+        close(dw, dww + old, dwe + 4 * U32 * old.abs(), "dweight accumulated")
+    # without the parameters' gradients; dx in place of dy
+    there = dy.clone()
+    ops.layer_norm_backward(there, x, w, mean, rstd, dx=there)
+    assert torch.equal(there, dx)
+
+
+def test_layer_norm_edges():
+    w = torch.ones((1, 64), device=DEV)
+    x = torch.full((1, 3, 64), 5.0, device=DEV)                     # no deviation: xh = 0 whatever eps is
+    y, mean, rstd = ops.layer_norm_forward(x, w, eps=1e-5)
+    assert bool((y == 0).all()) and bool((mean == 5).all())
+    x = randn(gen(5), 1, 8, 64)
+    x[0, 3, 7], x[0, 5, 1] = math.nan, math.inf                     # stay in their rows
+    y, *_ = ops.layer_norm_forward(x, w)
+    assert torch.isfinite(y).all(-1)[0].tolist() == [True, True, True, False, True, False, True, True]
+    keep = x.clone()
+    ops.layer_norm_forward(x, w, out=x)                             # in place
+    assert torch.equal(x.nan_to_num(0.0), ops.layer_norm_forward(keep, w)[0].nan_to_num(0.0))
+    empty = torch.empty((2, 0, 64), device=DEV)
+    y, mean, rstd = ops.layer_norm_forward(empty, torch.ones((2, 64), device=DEV))
+    dw = torch.ones((2, 64), device=DEV)
+    ops.layer_norm_backward(empty, empty, torch.ones((2, 64), device=DEV), mean, rstd, dw)
+    assert y.shape == (2, 0, 64) and bool((dw == 0).all())
+
+
+# ------------------------------------------------------------------------------------ attention
+def attn_want(q, k, v, cu, scale, dout=None):
+    """Definition in 64 bits, row sets by sequence; and sums of absolute terms for the bounds."""
+    T, H, D = q.shape
+    K = k.shape[1]
+    z = lambda n: torch.zeros((T, n, D), dtype=torch.float64, device=DEV)  # noqa: E731
+    r = dict(out=z(H), out_s=z(H), dq=z(H), dq_s=z(H), dk=z(K), dk_s=z(K), dv=z(K), dv_s=z(K),
+             lse=torch.full((H, T), -math.inf, dtype=torch.float64, device=DEV), z_s=torch.zeros((H, T), dtype=torch.float64, device=DEV))
+    for a, b in zip(cu, cu[1:]):
+        if a == b:
+            continue
+        see = torch.ones((b - a, b - a), dtype=torch.bool, device=DEV).tril()
+        for h in range(H):
+            g = h // (H // K)
+            qq, kk, vv = q[a:b, h].double(), k[a:b, g].double(), v[a:b, g].double()
+            s = (qq @ kk.T * scale).masked_fill(~see, -math.inf)
+            lse = torch.logsumexp(s, 1)
+            p = torch.exp(s - lse[:, None])
+            r["lse"][h, a:b] = lse
+            r["z_s"][h, a:b] = ((qq.abs() @ kk.abs().T) * abs(scale) * see).amax(1)
+            r["out"][a:b, h] = p @ vv
+            r["out_s"][a:b, h] = p @ vv.abs()
+            if dout is not None:
+                do = dout[a:b, h].double()
+                dp = do @ vv.T
+                delta = (p * dp).sum(1, keepdim=True)
+                dz = p * (dp - delta)
+                dps = p * (do.abs() @ vv.abs().T + (do.abs() * (p @ vv.abs())).sum(1, keepdim=True))
+                r["dv"][a:b, g] += p.T @ do
+                r["dv_s"][a:b, g] += p.T @ do.abs()
+                r["dq"][a:b, h] = dz @ kk * scale
+                r["dq_s"][a:b, h] = (dz.abs() + dps) @ kk.abs() * abs(scale)
+                r["dk"][a:b, g] += dz.T @ qq * scale
+                r["dk_s"][a:b, g] += (dz.abs() + dps).T @ qq.abs() * abs(scale)
+    return r
+
+
+def lengths(*n):
+    cu = [0]
+    for x in n:
+        cu.append(cu[-1] + x)
+    return cu
+
+
+ATTN = [  # cu_seqlens, tokens, heads, kv_heads, head_dim
+    (lengths(1), 1, 1, 1, 64),
+    (lengths(1, 1, 2, 0, 3), 7, 2, 1, 64),
+    (lengths(127), 127, 2, 2, 128),
+    (lengths(128, 129), 257, 2, 1, 128),
+    (lengths(300), 300, 8, 2, 64),
+    (lengths(5, 250, 0, 0, 256, 1, 257), 769, 4, 4, 128),
+    (lengths(100, 400), 600, 2, 2, 64),                     # 100 rows of no sequence at the end
+    (lengths(), 40, 2, 1, 64),                              # none but such rows
+    (lengths(513, 640), 1153, 6, 2, 80),
+    (lengths(90, 200), 290, 3, 3, 96),
+    (lengths(70, 60, 50), 180, 2, 1, 8),
+    (lengths(2000, 48), 2048, 4, 1, 128),
+    (lengths(*([3] * 200)), 600, 2, 2, 40),
+]
+
+
+@pytest.mark.parametrize("layout", ["own", "fused"])
+@pytest.mark.parametrize("cu,T,H,K,D", ATTN)
+def test_attention(cu, T, H, K, D, layout):
+    g = gen(T * D + H)
+    scale = 1.0 / math.sqrt(D)
+    if layout == "fused":
+        qkv = randn(g, T, H + 2 * K, D, dtype=BF16)
+        q, k, v = qkv[:, :H], qkv[:, H:H + K], qkv[:, H + K:]
+        grads = torch.full((T, H + 2 * K, D), 9.0, dtype=BF16, device=DEV)
+        dq, dk, dv = grads[:, :H], grads[:, H:H + K], grads[:, H + K:]
+    else:
+        # heads outermost: row stride D, head stride T * D
+        q, k, v = (randn(g, n, T, D, dtype=BF16).transpose(0, 1) for n in (H, K, K))
+        dq = dk = dv = None
+    q[cu[-1]:] = math.nan                                    # rows of no sequence may hold anything
+    k[cu[-1]:] = math.inf
+    v[cu[-1]:] = math.nan
+    dout = randn(g, T, H, D, dtype=BF16)
+    dout[cu[-1]:] = math.nan
+    cut = torch.tensor(cu, dtype=torch.int32, device=DEV)
+    out, check = guarded((T, H, D), BF16, DEV)
+    _, lse = ops.attention_forward(q, k, v, cut, out=out)
+    check()
+    want = attn_want(q[:cu[-1]], k[:cu[-1]], v[:cu[-1]], cu, scale, dout[:cu[-1]]) if cu[-1] else None
+    n = cu[-1]
+    assert bool((out[n:] == 0).all()) and bool((lse[:, n:] == -math.inf).all())
+    if n:
+        zs = want["z_s"]                                     # of the largest logit of each row
+        ze = 4 * math.sqrt(D) * U32 * zs
+        close(lse[:, :n], want["lse"], ze + 32 * U32 * (1 + want["lse"].abs()), "lse")
+        close(out[:n], want["out"], 2 * UBF * want["out_s"], "out")
+    dq, dk, dv = ops.attention_backward(dout, q, k, v, out, lse, cut, dq=dq, dk=dk, dv=dv)
+    for name, t in (("dq", dq), ("dk", dk), ("dv", dv)):
+        assert bool((t[n:] == 0).all()), name
+        if n:
+            close(t[:n], want[name], 2 * UBF * want[name + "_s"], name)
+    again = ops.attention_backward(dout, q, k, v, out, lse, cut)
+    for a, b in zip(again, (dq, dk, dv)):
+        assert torch.equal(a, b), "the same call twice"
+    ops.check_device_status()
+
+
+def test_attention_large_logits_and_scale():
+    """Logits of several hundred, a negative and a zero scale: the running maximum keeps everything finite."""
+    g = gen(77)
+    cu = lengths(200, 190)
+    q, k, v = (randn(g, 390, 2, 64, dtype=BF16, std=s) for s in (8.0, 8.0, 1.0))
+    cut = torch.tensor(cu, dtype=torch.int32, device=DEV)
+    for scale in (1.0, -0.5, 0.0):
+        out, lse = ops.attention_forward(q, k, v, cut, scale=scale)
+        want = attn_want(q, k, v, cu, scale)
+        ze = 4 * math.sqrt(64) * U32 * want["z_s"]
+        close(lse, want["lse"], ze + 32 * U32 * (1 + want["lse"].abs()), f"lse, scale {scale}")
+        # a logit's error is a relative error of its exponential
+        close(out, want["out"], (2 * UBF + 2 * ze.amax()) * want["out_s"], f"out, scale {scale}")
+
+
+@pytest.mark.parametrize("D,H,K", [(64, 2, 1), (128, 2, 2)])
+@pytest.mark.parametrize("where,value", [("v", math.inf), ("v", math.nan), ("k", math.nan), ("k", math.inf), ("q", math.nan), ("dout", math.inf)])
+def test_attention_hidden_rows_stay_hidden(where, value, D, H, K):
+    """A row that a query does not see never reaches it: later tokens of its sequence, other sequences; and the
+    gradient of a key has nothing of rows that do not see it."""
+    g = gen(5)
+    cu = lengths(150, 300)
+    bad = 150 + 170                                           # in the middle of the second sequence
+    t = dict(q=randn(g, 450, H, D, dtype=BF16), k=randn(g, 450, K, D, dtype=BF16), v=randn(g, 450, K, D, dtype=BF16),
+             dout=randn(g, 450, H, D, dtype=BF16))
+    cut = torch.tensor(cu, dtype=torch.int32, device=DEV)
+    out0, lse0 = ops.attention_forward(t["q"], t["k"], t["v"], cut)
+    g0 = ops.attention_backward(t["dout"], t["q"], t["k"], t["v"], out0, lse0, cut)
+    t[where][bad] = value
+    out, lse = ops.attention_forward(t["q"], t["k"], t["v"], cut)
+    dq, dk, dv = ops.attention_backward(t["dout"], t["q"], t["k"], t["v"], out, lse, cut)
+    scale = D ** -0.5
+    seen = torch.ones(450, dtype=torch.bool, device=DEV)      # rows whose output cannot depend on row `bad`
+    if where in ("k", "v"):
+        seen[bad:] = False
+    elif where == "q":
+        seen[bad] = False
+    want = attn_want(t["q"][:150], t["k"][:150], t["v"][:150], [0, 150], scale)
+    close(out[:150], want["out"], 2 * UBF * want["out_s"], "the first sequence")
+    close(out[seen], out0[seen].double(), 2.0 ** -7 * out0[seen].double().abs() + 4 * UBF, "rows that do not see it")
+    close(lse[:, seen], lse0[:, seen].double(), 32 * U32 * (1 + lse0[:, seen].double().abs()), "lse")
+    if where in ("k", "v"):
+        assert not bool(torch.isfinite(out[bad:]).all(-1).all(-1).any()) or value == math.inf and where == "k"
+    # gradients: queries before `bad` never see it; keys after it are not seen by it
+    early = torch.zeros(450, dtype=torch.bool, device=DEV)
+    early[:bad] = True
+    after = torch.ones(450, dtype=torch.bool, device=DEV)
+    after[150:bad + 1] = False
+    if where in ("k", "v"):
+        after[bad:] = False                                   # rows after it see it: their gradients may be anything
+        assert bool(torch.isfinite(dq[early]).all())
+        close(dq[early], g0[0][early].double(), 2.0 ** -6 * g0[0][early].double().abs() + 8 * UBF, "dq")
+    else:
+        rest = torch.ones(450, dtype=torch.bool, device=DEV)
+        rest[bad] = False
+        close(dq[rest], g0[0][rest].double(), 2.0 ** -6 * g0[0][rest].double().abs() + 8 * UBF, "dq")
+    for t0, t1, name in ((g0[1], dk, "dk"), (g0[2], dv, "dv")):
+        close(t1[after], t0[after].double(), 2.0 ** -6 * t0[after].double().abs() + 16 * UBF, name)
+    ops.check_device_status()
+
+
+# ----------------------------------------------------------------------------------------- loss
+DISTILL = [  # rows, vocab, k, logits, teacher, temperature, z, id type
+    (1, 1, 1, F32, F32, 1.0, 0.0, torch.int32),
+    (5, 7, 3, F32, F32, 2.0, 1e-2, torch.int64),
+    (24, 32000, 1, F32, F32, 1.0, 1e-4, torch.int32),
+    (33, 32000, 64, BF16, BF16, 2.0, 0.0, torch.int32),
+    (19, 50021, 64, BF16, BF16, 1.5, 1e-4, torch.int32),      # rows start anywhere within 16 bytes
+    (13, 2003, 100, F32, BF16, 1.0, 0.0, torch.int64),
+    (7, 8191, 20, BF16, F32, 0.7, 1e-3, torch.int32),
+    (3, 200003, 1000, BF16, BF16, 1.0, 0.0, torch.int32),     # longer than a block holds
+    (3, 70001, 5, F32, F32, 3.0, 1e-4, torch.int32),
+    (300, 130, 130, F32, F32, 1.0, 0.0, torch.int32),
+]
+
+
+def distill_want(x, ids, t, T, z, w):
+    x, t, w = x.double(), t.double(), w.double()
+    V = x.shape[1]
+    keep = (ids >= 0) & (ids < V)
+    at = ids.long().clamp(0, V - 1)
+    lse = torch.logsumexp(x / T, 1)
+    some = keep.any(1)
+    p = torch.softmax(torch.where(keep, t / T, torch.full_like(t, -1e300)), 1) * keep
+    logq = x.gather(1, at) / T - lse[:, None]
+    terms = torch.special.xlogy(p, p) - torch.where(p > 0, p * logq, torch.zeros_like(p))
+    loss = w * some * (T * T * terms.sum(1) + z * lse * lse)
+    q = torch.exp(x / T - lse[:, None])
+    wq = (w * some)[:, None]
+    grad = wq * q * (T + 2 * z * lse / T)[:, None]
+    grad = grad.scatter_add(1, at, -wq * T * p)
+    size = w.abs() * (T * T * terms.abs().sum(1) + z * lse * lse)
+    return loss, lse, grad, size, p, q, wq
+
+
+@pytest.mark.parametrize("N,V,k,dt,tdt,T,z,idt", DISTILL)
+def test_distill(N, V, k, dt, tdt, T, z, idt):
+    g = gen(N + V + k)
+    x = randn(g, N, V, dtype=dt, std=3.0)
+    ids = torch.randint(0, V, (N, k), generator=g, device=DEV).to(idt)     # ids appear twice here and there
+    t = randn(g, N, k, dtype=tdt, std=2.0)
+    if N > 4:
+        ids[1] = -1                                                        # a row without a teacher
+        ids[2, k // 2:] = V                                                # unused entries
+        ids[3] = ids[3, 0].clone()                                                 # one id in all places
+        x[4, V // 2:] = -math.inf                                          # a masked part of the vocabulary
+        ids[4] %= max(V // 2, 1)
+    w = torch.rand(N, generator=g, device=DEV) + 0.5
+    loss, lse, _ = ops.distill_loss(x, ids, t, temperature=T, z_coef=z, row_weight=w)
+    want = distill_want(x, ids, t, T, z, w)
+    zs = x.double().nan_to_num(0, 0, 0).abs().amax(1) / T                  # size of what is exponentiated
+    le = U32 * (16 + 4 * math.sqrt(V) + 8 * zs)                            # relative error of a sum of exponentials
+    close(lse, want[1], le + 4 * U32 * want[1].abs(), "lse")
+    close(loss, want[0], want[3] * (4 * math.sqrt(k) + 16) * U32 + w.double() * (T * T + 2 * z * want[1].abs()) * (le + 8 * U32 * (want[1].abs() + zs + 1)) * 2, "loss")
+    grad, check = guarded((N, V), dt, DEV)
+    loss2, lse2, _ = ops.distill_loss(x, ids, t, temperature=T, z_coef=z, row_weight=w, dlogits=grad)
+    check()
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2)
+    q, wq = want[5], want[6]
+    pe = (16 + 4 * math.sqrt(k) + 8 * t.double().abs().amax(1) / T) * U32
+    mass = torch.zeros_like(q).scatter_add_(1, ids.long().clamp(0, V - 1), want[4])
+    bound = wq * (q * (T + 2 * z * want[1].abs() / T)[:, None] * 2 * (le[:, None] + 8 * U32 * (1 + zs[:, None])) + T * mass * 2 * pe[:, None])
+    close(grad, want[2], bound + 1e-37, "dlogits")
+    # a stride of its own (another place within 16 bytes), and in place
+    apart = torch.full((N, V + 3), 5.0, dtype=dt, device=DEV)
+    ops.distill_loss(x, ids, t, temperature=T, z_coef=z, row_weight=w, dlogits=apart[:, :V])
+    close(apart[:, :V], want[2], bound + 1e-37, "dlogits at another stride")
+    assert bool((apart[:, V:] == 5.0).all())
+    here = x.clone()
+    ops.distill_loss(here, ids, t, temperature=T, z_coef=z, row_weight=w, dlogits=here)
+    assert torch.equal(here, grad), "in place"
+
+
+def test_distill_no_rows_and_scale():
+    x = randn(gen(1), 0, 50)
+    loss, lse, grad = ops.distill_loss(x, torch.zeros((0, 2), dtype=torch.int32, device=DEV), torch.zeros((0, 2), device=DEV), grad=True)
+    assert loss.shape == (0,) and grad.shape == (0, 50)
+    x = randn(gen(1), 6, 50)
+    ids = torch.arange(6, device=DEV, dtype=torch.int32)[:, None]
+    a = ops.distill_loss(x, ids, torch.zeros((6, 1), device=DEV), grad=True)
+    b = ops.distill_loss(x, ids, torch.full((6, 1), 40.0, device=DEV), grad=True, grad_scale=0.5)
+    want = torch.nn.functional.cross_entropy(x.double(), ids[:, 0].long(), reduction="none")
+    close(a[0], want, 64 * U32 * (1 + want), "cross-entropy")
+    assert torch.equal(a[0] * 0.5, b[0]) and torch.equal(a[2] * 0.5, b[2])
+
+
+# ------------------------------------------------------------------------ differences and autograd
+def test_gradients_against_differences():
+    """Central differences of the forward calls in fp32: the truncation error h^2 |f'''| and the rounding error
+    u |f| / h are both below 3e-3 of the gradients' size at h = 2^-6 with values near one."""
+    g = gen(11)
+    h = 2.0 ** -6
+
+    def slope(f, t, direction):
+        return (f(t + h * direction) - f(t - h * direction)).double() / (2 * h)
+
+    x, w, b, r = randn(g, 1, 6, 40), randn(g, 1, 40, mean=1.0, std=0.2), randn(g, 1, 40), randn(g, 1, 6, 40)
+    _, mean, rstd = ops.layer_norm_forward(x, w, b)
+    dw, db = torch.empty_like(w), torch.empty_like(b)
+    dx = ops.layer_norm_backward(r, x, w, mean, rstd, dw, db)
+    f = lambda x_, w_, b_: (ops.layer_norm_forward(x_, w_, b_)[0] * r).double().sum()  # noqa: E731
+    for t, grad, call in ((x, dx, lambda t_: f(t_, w, b)), (w, dw, lambda t_: f(x, t_, b)), (b, db, lambda t_: f(x, w, t_))):
+        for _ in range(4):
+            d = randn(g, *t.shape)
+            d /= d.norm()
+            assert abs(float(slope(call, t, d) - (grad.double() * d).sum())) <= 1e-2 * float(grad.norm())
+    z = randn(g, 5, 37)
+    ids, t = torch.randint(0, 37, (5, 4), generator=g, device=DEV, dtype=torch.int32), randn(g, 5, 4)
+    how = dict(temperature=1.5, z_coef=1e-2)
+    grad = ops.distill_loss(z, ids, t, grad=True, **how)[2]
+    for _ in range(4):
+        d = randn(g, 5, 37)
+        d /= d.norm()
+        got = slope(lambda z_: ops.distill_loss(z_, ids, t, **how)[0].double().sum(), z, d)
+        assert abs(float(got - (grad.double() * d).sum())) <= 1e-2 * float(grad.norm())
+
+
+def test_attention_gradient_against_differences():
+    """The same in bf16: the output's rounding (2^-9 of about one, over 3 * 70 * 64 random elements) leaves
+    2^-9 sqrt(13440) / (2 h |d|) of noise against a slope of size |grad|: a long step along the gradient itself and
+    5 % of tolerance."""
+    g = gen(12)
+    cut = torch.tensor([0, 30, 70], dtype=torch.int32, device=DEV)
+    t = [randn(g, 70, n, 64, dtype=BF16) for n in (4, 2, 2)]
+    r = randn(g, 70, 4, 64, dtype=BF16)
+    out, lse = ops.attention_forward(*t, cut)
+    grads = ops.attention_backward(r, *t, out, lse, cut)
+    f = lambda ts: (ops.attention_forward(*ts, cut)[0].double() * r.double()).sum()  # noqa: E731
+    for i in range(3):
+        d = grads[i].double() / grads[i].double().norm()
+        step = 2.0
+        up, down = list(t), list(t)
+        up[i], down[i] = (t[i].double() + step * d).to(BF16), (t[i].double() - step * d).to(BF16)
+        moved = (up[i].double() - down[i].double())
+        got = float(f(up) - f(down))
+        assert abs(got - float((grads[i].double() * moved).sum())) <= 0.05 * float(grads[i].double().norm()) * float(moved.norm())
+
+
+def test_autograd_forms():
+    g = gen(13)
+    ids = torch.randint(0, 50, (2, 40), generator=g, device=DEV, dtype=torch.int32)
+    table = randn(g, 2, 50, 64).requires_grad_()
+    w, b = randn(g, 2, 64, mean=1.0).requires_grad_(), randn(g, 2, 64).requires_grad_()
+    cut = torch.tensor([0, 50, 80], dtype=torch.int32, device=DEV)
+    x = ops.layer_norm(ops.embedding(ids, table, scale=8.0), w, b)
+    q = x.to(BF16).view(80, 1, 64).expand(80, 2, 64)
+    o = ops.attention(q, q[:, :1], q[:, 1:], cut)
+    loss = ops.distill(o.float().reshape(160, 64), torch.arange(160, device=DEV, dtype=torch.int32)[:, None] % 64, torch.zeros((160, 1), device=DEV)).mean()
+    loss.backward()
+    # the same in torch's operators
+    t2, w2, b2 = (p.detach().clone().requires_grad_() for p in (table, w, b))
+    x2 = torch.stack([torch.nn.functional.layer_norm(t2[m][ids[m].long()] * 8.0, (64,), w2[m], b2[m]) for m in range(2)])
+    q2 = x2.to(BF16).float().view(80, 1, 64)
+    see = (torch.ones(80, 80, device=DEV).tril() * (torch.arange(80, device=DEV)[:, None] >= 50).eq(torch.arange(80, device=DEV)[None] >= 50)).bool()
+    a2 = torch.softmax((q2[:, 0] @ q2[:, 0].T / 8.0).masked_fill(~see, -math.inf), -1) @ q2[:, 0]
+    o2 = a2[:, None].expand(80, 2, 64).reshape(160, 64)
+    loss2 = torch.nn.functional.cross_entropy(o2, torch.arange(160, device=DEV) % 64)
+    loss2.backward()
+    assert abs(float(loss - loss2)) < 2e-2
+    for p, p2 in ((table, t2), (w, w2), (b, b2)):
+        # bf16 activations and gradients in the middle: a few roundings of 2^-9 each
+        assert float((p.grad - p2.grad).norm()) <= 0.03 * float(p2.grad.norm())
+
+
+# --------------------------------------------------------------------- streams, graphs, refusals
+def test_other_stream_and_graph():
+    """Launched on a stream of the caller's while its tensors belong to another, and replayed from a graph."""
+    g = gen(21)
+    T = 500
+    cut = torch.tensor([0, 200, T], dtype=torch.int32, device=DEV)
+    qkv, dout = randn(g, T, 6, 64, dtype=BF16), randn(g, T, 2, 64, dtype=BF16)
+    ids = torch.randint(0, 1000, (2, 3000), generator=g, device=DEV, dtype=torch.int32)
+    rows, x, w = randn(g, 2, 3000, 64), randn(g, 2, 3000, 64), randn(g, 2, 64)
+    z = randn(g, 64, 1000)
+    tid, tl = torch.randint(0, 1000, (64, 8), generator=g, device=DEV, dtype=torch.int32), randn(g, 64, 8)
+
+    def everything(**kw):
+        q, k, v = qkv[:, :2], qkv[:, 2:4], qkv[:, 4:]
+        out, lse = ops.attention_forward(q, k, v, cut, **kw)
+        grads = ops.attention_backward(dout, q, k, v, out, lse, cut, **kw)
+        dtable = ops.embedding_backward(ids, rows, torch.empty((2, 1000, 64), device=DEV), **kw)
+        y, mean, rstd = ops.layer_norm_forward(x, w, **kw)
+        dw = torch.empty_like(w)
+        dx = ops.layer_norm_backward(rows, x, w, mean, rstd, dw, **kw)
+        loss, l2, dz = ops.distill_loss(z, tid, tl, grad=True, **kw)
+        return (out, lse) + grads + (dtable, y, dx, dw, loss, dz)
+
+    want = everything()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = everything(stream=side)
+    side.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = everything()
+    for t in got:
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+def test_refusals():
+    g = gen(31)
+    lib = binding.load_library()
+    ids = torch.zeros((1, 4), dtype=torch.int32, device=DEV)
+    table = randn(g, 1, 10, 16)
+    n0 = binding.launch_count()
+    with pytest.raises(TypeError):
+        ops.embedding_forward(ids.float(), table)
+    with pytest.raises(TypeError):
+        ops.embedding_forward(ids, table.half())
+    with pytest.raises(ValueError):
+        ops.embedding_forward(ids, table.cpu())
+    with pytest.raises(ValueError):
+        ops.embedding_forward(ids, table[0])
+    with pytest.raises(ValueError):
+        ops.embedding_backward(ids, table.new_zeros((1, 5, 16)), table.clone())
+    with pytest.raises(binding.DilocoError) as e:
+        ops.embedding_forward(ids, torch.empty((1, (1 << 20) + 1, 1), device=DEV))
+    assert e.value.status == binding.ERR_UNSUPPORTED
+    x, w = randn(g, 1, 4, 64), randn(g, 1, 64)
+    with pytest.raises(ValueError):
+        ops.layer_norm_forward(x, w[:, :32])
+    with pytest.raises(ValueError):
+        ops.layer_norm_forward(x.transpose(1, 2), w[:, :4])
+    with pytest.raises(binding.DilocoError) as e:
+        ops.layer_norm_forward(x, w, eps=-1.0)
+    assert e.value.status == binding.ERR_INVALID_ARG
+    cut = torch.tensor([0, 8], dtype=torch.int32, device=DEV)
+    q, kv = randn(g, 8, 4, 64, dtype=BF16), randn(g, 8, 2, 64, dtype=BF16)
+    with pytest.raises(TypeError):
+        ops.attention_forward(q.float(), kv, kv, cut)
+    with pytest.raises(TypeError):
+        ops.attention_forward(q, kv, kv, cut.long())
+    with pytest.raises(ValueError):
+        ops.attention_forward(q, kv, kv[:4], cut)
+    for bad, status in ((randn(g, 8, 3, 64, dtype=BF16), binding.ERR_INVALID_ARG),):
+        with pytest.raises(binding.DilocoError) as e:
+            ops.attention_forward(q, bad, bad, cut)
+        assert e.value.status == status
+    for D in (60, 136):
+        t = randn(g, 8, 2, D, dtype=BF16)
+        with pytest.raises(binding.DilocoError) as e:
+            ops.attention_forward(t, t, t, cut)
+        assert e.value.status == binding.ERR_UNSUPPORTED
+    odd = randn(g, 8, 2, 68, dtype=BF16)[:, :, 4:]              # starts 8 bytes into a 16-byte unit
+    with pytest.raises(binding.DilocoError) as e:
+        ops.attention_forward(odd, odd, odd, cut)
+    assert e.value.status == binding.ERR_MISALIGNED
+    z = randn(g, 4, 9)
+    with pytest.raises(binding.DilocoError) as e:
+        ops.distill_loss(z, torch.zeros((4, 1), dtype=torch.int32, device=DEV), torch.zeros((4, 1), device=DEV), temperature=0.0)
+    assert e.value.status == binding.ERR_INVALID_ARG
+    with pytest.raises(binding.DilocoError) as e:
+        ops.distill_loss(z, torch.zeros((4, 1025), dtype=torch.int32, device=DEV), torch.zeros((4, 1025), device=DEV))
+    assert e.value.status == binding.ERR_UNSUPPORTED
+    with pytest.raises(ValueError):
+        ops.distill_loss(z, torch.zeros((3, 1), dtype=torch.int32, device=DEV), torch.zeros((3, 1), device=DEV))
+    # the C calls themselves: a host pointer, too small a workspace
+    host = torch.zeros(64)
+    e = binding.Embedding(1, 16, 4, 10, 160, 160, 16, 1.0, 0, 0, 0, 0)
+    assert lib.diloco_embedding_forward(ctypes.byref(e), ids.data_ptr(), host.data_ptr(), table.data_ptr(), None) == binding.ERR_INVALID_ARG
+    assert lib.diloco_embedding_backward(ctypes.byref(e), ids.data_ptr(), table.data_ptr(), table.data_ptr(), 0, table.data_ptr(), 16, None) in (
+        binding.ERR_INVALID_ARG, binding.ERR_MISALIGNED)
+    assert binding.launch_count() == n0
+    torch.cuda.synchronize()

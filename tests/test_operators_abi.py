@@ -1,0 +1,87 @@
+"""The operators' C calls refuse bad descriptors and null pointers before they touch a device (no GPU needed)."""
+import ctypes
+
+import pytest
+
+from paper_2502_12996_b200 import binding, build
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build_library()
+    return binding.load_library()
+
+
+def embedding(**kw):
+    d = dict(M=2, d=16, tokens=5, vocab=10, table_stride=160, grad_stride=160, row_stride=16, scale=1.0)
+    return binding.Embedding(**{**d, **kw})
+
+
+def norm(**kw):
+    d = dict(M=2, d=16, groups=1, rows=5, x_row_stride=16, y_row_stride=16, dx_row_stride=16, param_stride=16, grad_stride=16, eps=1e-5)
+    return binding.LayerNorm(**{**d, **kw})
+
+
+def attention(**kw):
+    d = dict(heads=4, kv_heads=2, head_dim=64, sequences=1, tokens=8, scale=1.0)
+    for t in ("q", "k", "v", "o", "do", "dq", "dk", "dv"):
+        d[f"{t}_row_stride"], d[f"{t}_head_stride"] = 256, 64
+    return binding.Attention(**{**d, **kw})
+
+
+def distill(**kw):
+    d = dict(rows=3, vocab=7, logits_stride=7, grad_stride=7, k=2, temperature=1.0, z_coef=0.0, grad_scale=1.0)
+    return binding.Distill(**{**d, **kw})
+
+
+INV, UNS, MIS = binding.ERR_INVALID_ARG, binding.ERR_UNSUPPORTED, binding.ERR_MISALIGNED
+
+
+@pytest.mark.parametrize("kw,status", [(dict(M=0), INV), (dict(d=0), INV), (dict(tokens=-1), INV), (dict(vocab=0), INV), (dict(row_stride=15), INV),
+                                       (dict(ids_int64=2), INV), (dict(table_dtype=2), INV), (dict(act_dtype=-1), INV), (dict(grad_dtype=3), INV),
+                                       (dict(table_stride=159), INV), (dict(vocab=(1 << 20) + 1), UNS), (dict(tokens=1 << 31), UNS)])
+def test_embedding_descriptor(lib, kw, status):
+    e = embedding(**kw)
+    assert lib.diloco_embedding_forward(ctypes.byref(e), None, None, None, None) == status
+    assert lib.diloco_embedding_workspace_bytes(ctypes.byref(e)) == status
+    assert lib.diloco_embedding_backward(ctypes.byref(e), None, None, None, 0, None, 0, None) == status
+
+
+@pytest.mark.parametrize("kw,status", [(dict(M=0), INV), (dict(d=0), INV), (dict(rows=-1), INV), (dict(groups=0), INV), (dict(x_row_stride=-1), INV),
+                                       (dict(eps=-1.0), INV), (dict(eps=float("nan")), INV), (dict(act_dtype=2), INV), (dict(param_stride=15), INV),
+                                       (dict(d=65537, param_stride=65537, grad_stride=65537), UNS), (dict(rows=1 << 31), UNS)])
+def test_layernorm_descriptor(lib, kw, status):
+    n = norm(**kw)
+    assert lib.diloco_layernorm_forward(ctypes.byref(n), *[None] * 7) == status
+    assert lib.diloco_layernorm_backward(ctypes.byref(n), *[None] * 8, 0, None, 0, None) == status
+
+
+@pytest.mark.parametrize("kw,status", [(dict(heads=3), INV), (dict(kv_heads=0), INV), (dict(head_dim=0), INV), (dict(tokens=-1), INV),
+                                       (dict(sequences=-1), INV), (dict(scale=float("inf")), INV), (dict(q_row_stride=-8), INV),
+                                       (dict(head_dim=12), UNS), (dict(head_dim=136), UNS), (dict(tokens=(1 << 24) + 1), UNS),
+                                       (dict(v_head_stride=60), MIS), (dict(o_row_stride=252), MIS)])
+def test_attention_descriptor(lib, kw, status):
+    a = attention(**kw)
+    assert lib.diloco_attention_forward(ctypes.byref(a), *[None] * 7) == status
+    assert lib.diloco_attention_backward(ctypes.byref(a), *[None] * 11, 0, None) == status
+
+
+@pytest.mark.parametrize("kw,status", [(dict(rows=-1), INV), (dict(vocab=0), INV), (dict(k=0), INV), (dict(logits_stride=6), INV), (dict(dtype=5), INV),
+                                       (dict(temperature=0.0), INV), (dict(temperature=float("inf")), INV), (dict(z_coef=-1.0), INV),
+                                       (dict(grad_scale=float("nan")), INV), (dict(k=1025), UNS), (dict(vocab=1 << 31, logits_stride=1 << 31), UNS)])
+def test_distill_descriptor(lib, kw, status):
+    l = distill(**kw)
+    assert lib.diloco_distill_loss(ctypes.byref(l), *[None] * 8) == status
+
+
+def test_null_and_empty(lib):
+    assert lib.diloco_embedding_forward(None, *[None] * 4) == INV
+    assert lib.diloco_layernorm_forward(None, *[None] * 7) == INV
+    assert lib.diloco_attention_forward(None, *[None] * 7) == INV
+    assert lib.diloco_distill_loss(None, *[None] * 8) == INV
+    # nothing to do is no error, and needs no pointer
+    assert lib.diloco_embedding_forward(ctypes.byref(embedding(tokens=0)), *[None] * 4) == 0
+    assert lib.diloco_layernorm_forward(ctypes.byref(norm(rows=0)), *[None] * 7) == 0
+    assert lib.diloco_attention_forward(ctypes.byref(attention(tokens=0)), *[None] * 7) == 0
+    assert lib.diloco_distill_loss(ctypes.byref(distill(rows=0)), *[None] * 8) == 0
+    assert lib.diloco_check_status_word(None, None) == 0
