@@ -323,6 +323,12 @@ EncodeTiledFn encode_tiled_fn() {
   return fn;
 }
 
+} // namespace
+
+void *diloco::tensor_map_encoder() { return reinterpret_cast<void *>(encode_tiled_fn()); }
+
+namespace {
+
 // fp32 tensor [rows, cols] with row pitch `pitch` elements, boxes of [rows, T]
 int encode_rows(CUtensorMap *map, float *base, int64_t cols, int rows, int64_t pitch, int T) {
   EncodeTiledFn fn = encode_tiled_fn();

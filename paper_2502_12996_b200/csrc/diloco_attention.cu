@@ -1,24 +1,41 @@
 // Causal attention over packed sequences with grouped heads: host side, and the row-at-a-time kernels.
 #include "diloco_attention_rows.cuh"
+#include "diloco_tcgen05.cuh"
 
 namespace diloco {
+
+int attn_forward(const AttnArgs &a, cudaStream_t s);
+void *tensor_map_encoder();
+
+// [tokens, heads, head_dim] as 3-D boxes of 64 columns, one head and box_rows tokens, 128-byte swizzled.
+int encode_heads(HeadMap *m, const void *base, int head_dim, int heads, long long head_stride, long long tokens, long long row_stride,
+                 int box_rows) {
+  using Fn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                          const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                          CUtensorMapFloatOOBfill);
+  const Fn fn = reinterpret_cast<Fn>(tensor_map_encoder());
+  if (!fn) return DILOCO_ERR_UNSUPPORTED;
+  m->head_mul = head_stride == 0 ? 0 : 1; // one head for all: its axis has one element
+  if (head_stride == 0) heads = 1, head_stride = head_dim;
+  m->token_last = row_stride >= head_stride;
+  const int t = m->token_last ? 2 : 1, hd = 3 - t;
+  cuuint64_t dims[3] = {(cuuint64_t)head_dim}, strides[2];
+  cuuint32_t box[3] = {64};
+  const cuuint32_t one[3] = {1, 1, 1};
+  dims[t] = (cuuint64_t)tokens, dims[hd] = (cuuint64_t)heads;
+  strides[t - 1] = (cuuint64_t)row_stride * 2, strides[hd - 1] = (cuuint64_t)head_stride * 2;
+  box[t] = (cuuint32_t)box_rows, box[hd] = 1;
+  const CUresult r = fn(&m->map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, one,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? DILOCO_OK : DILOCO_ERR_UNSUPPORTED;
+}
+
 namespace {
 
 constexpr int kRowWarps = 8;
 
 // One warp for each row (blockIdx.x * 8 + warp) of head blockIdx.y.
-__global__ void __launch_bounds__(32 * kRowWarps, 1) attn_forward_rows_kernel(const AttnArgs a) {
-  const int i = blockIdx.x * kRowWarps + (threadIdx.x >> 5), h = blockIdx.y, lane = threadIdx.x & 31;
-  if (i >= a.tokens) return;
-  int first, end;
-  sequence_of(a, i, first, end);
-  if (first >= 0) attn_out_row(a, i, h, first, lane);
-  else {
-    for (int c = lane; c < a.head_dim; c += 32) a.out[i * a.o_row + h * a.o_head + c] = __float2bfloat16_rn(0.f);
-    if (lane == 0) a.lse[(long long)h * a.tokens + i] = -INFINITY;
-  }
-}
-
 __global__ void __launch_bounds__(32 * kRowWarps, 1) attn_dq_rows_kernel(const AttnArgs a) {
   const int i = blockIdx.x * kRowWarps + (threadIdx.x >> 5), h = blockIdx.y, lane = threadIdx.x & 31;
   if (i >= a.tokens) return;
@@ -42,7 +59,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) attn_dkv_rows_kernel(const 
     }
 }
 
-bool stride_ok(int64_t row, int64_t head) { return row >= 0 && head >= 0; }
+bool stride_ok(int64_t row, int64_t head) { return row > 0 && head >= 0; }
 bool stride_wide(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
 
 int valid(const diloco_attention_t *a, bool backward) {
@@ -98,8 +115,7 @@ int diloco_attention_forward(const diloco_attention_t *d, const void *q, const v
   if (pc.rc != DILOCO_OK) return pc.rc;
   AttnArgs a = args_of(d, q, k, v, cu_seqlens);
   a.out = static_cast<__nv_bfloat16 *>(out), a.lse = lse;
-  attn_forward_rows_kernel<<<dim3((a.tokens + kRowWarps - 1) / kRowWarps, a.heads), 32 * kRowWarps, 0, static_cast<cudaStream_t>(stream)>>>(a);
-  return launched();
+  return attn_forward(a, static_cast<cudaStream_t>(stream));
 }
 
 int64_t diloco_attention_workspace_bytes(const diloco_attention_t *d) {

@@ -14,6 +14,7 @@ namespace diloco {
 int cuda_fail(cudaError_t e);
 void count_launch();
 int check_device_pointer(const void *p, int device);
+void *tensor_map_encoder(); // cuTensorMapEncodeTiled, nullptr where the driver has none
 
 // The one (variant, theta storage) -> template-argument ladder: f is called with two
 // std::integral_constant tags.
