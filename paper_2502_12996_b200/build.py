@@ -12,7 +12,8 @@ LIB = PKG / "libdiloco.so"
 REPORT = PKG / "ptxas_report.txt"        # registers / spills of every kernel, written by each build
 OUTER_M = [0, 1, 2, 3, 4, 8, 16, 1000, 1002, 1003, 1004]   # translation units: replica counts with kernels of their own, the
                                                  # warp-split forms (1000, 1002) and the first-steps form (0)
-OPERATORS = ["diloco_embedding", "diloco_layernorm", "diloco_distill", "diloco_attention", "diloco_attention_fwd"]   # units of the decoder operators
+# units of the decoder operators
+OPERATORS = ["diloco_embedding", "diloco_layernorm", "diloco_distill", "diloco_attention", "diloco_attention_fwd", "diloco_attention_bwd"]
 OBJ = PKG / "_obj"
 
 NVCC_FLAGS = [

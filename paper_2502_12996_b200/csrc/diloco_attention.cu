@@ -1,10 +1,12 @@
-// Causal attention over packed sequences with grouped heads: host side, and the row-at-a-time kernels.
+// Causal attention over packed sequences with grouped heads: host side.  The kernels are in
+// diloco_attention_fwd.cu and diloco_attention_bwd.cu.
 #include "diloco_attention_rows.cuh"
 #include "diloco_tcgen05.cuh"
 
 namespace diloco {
 
 int attn_forward(const AttnArgs &a, cudaStream_t s);
+int attn_backward(const AttnArgs &a, cudaStream_t s);
 void *tensor_map_encoder();
 
 // [tokens, heads, head_dim] as 3-D boxes of 64 columns, one head and box_rows tokens, 128-byte swizzled.
@@ -32,32 +34,6 @@ int encode_heads(HeadMap *m, const void *base, int head_dim, int heads, long lon
 }
 
 namespace {
-
-constexpr int kRowWarps = 8;
-
-// One warp for each row (blockIdx.x * 8 + warp) of head blockIdx.y.
-__global__ void __launch_bounds__(32 * kRowWarps, 1) attn_dq_rows_kernel(const AttnArgs a) {
-  const int i = blockIdx.x * kRowWarps + (threadIdx.x >> 5), h = blockIdx.y, lane = threadIdx.x & 31;
-  if (i >= a.tokens) return;
-  int first, end;
-  sequence_of(a, i, first, end);
-  if (first >= 0) attn_dq_row(a, i, h, first, lane);
-  else
-    for (int c = lane; c < a.head_dim; c += 32) a.dq[i * a.dq_row + h * a.dq_head + c] = __float2bfloat16_rn(0.f);
-}
-
-__global__ void __launch_bounds__(32 * kRowWarps, 1) attn_dkv_rows_kernel(const AttnArgs a) {
-  const int j = blockIdx.x * kRowWarps + (threadIdx.x >> 5), g = blockIdx.y, lane = threadIdx.x & 31;
-  if (j >= a.tokens) return;
-  int first, end;
-  sequence_of(a, j, first, end);
-  if (first >= 0) attn_dkv_row(a, j, g, end, lane);
-  else
-    for (int c = lane; c < a.head_dim; c += 32) {
-      a.dk[j * a.dk_row + g * a.dk_head + c] = __float2bfloat16_rn(0.f);
-      a.dv[j * a.dv_row + g * a.dv_head + c] = __float2bfloat16_rn(0.f);
-    }
-}
 
 bool stride_ok(int64_t row, int64_t head) { return row > 0 && head >= 0; }
 bool stride_wide(int64_t row, int64_t head) { return row % 8 == 0 && head % 8 == 0; }
@@ -138,13 +114,7 @@ int diloco_attention_backward(const diloco_attention_t *d, const void *dout, con
   a.dout = static_cast<const __nv_bfloat16 *>(dout), a.out_in = static_cast<const __nv_bfloat16 *>(out);
   a.lse = const_cast<float *>(lse), a.delta = static_cast<float *>(workspace);
   a.dq = static_cast<__nv_bfloat16 *>(dq), a.dk = static_cast<__nv_bfloat16 *>(dk), a.dv = static_cast<__nv_bfloat16 *>(dv);
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int blocks = (a.tokens + kRowWarps - 1) / kRowWarps;
-  attn_dq_rows_kernel<<<dim3(blocks, a.heads), 32 * kRowWarps, 0, s>>>(a);
-  rc = launched();
-  if (rc != DILOCO_OK) return rc;
-  attn_dkv_rows_kernel<<<dim3(blocks, a.kv_heads), 32 * kRowWarps, 0, s>>>(a);
-  return launched();
+  return attn_backward(a, static_cast<cudaStream_t>(stream));
 }
 
 } // extern "C"

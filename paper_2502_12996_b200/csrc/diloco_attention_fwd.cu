@@ -15,13 +15,11 @@
 // Tiles of a sequence that start together on both axes need a mask on the diagonal tile alone.  V rows behind the
 // sequence's end are zeroed in shared memory (0 * NaN); a row that comes out non-finite all the same is computed
 // again over the rows that it sees alone, so that a later token's NaN cannot reach an earlier one.
-#include "diloco_attention_rows.cuh"
-#include "diloco_tcgen05.cuh"
+#include "diloco_attention_tiles.cuh"
 
 namespace diloco {
 namespace {
 
-constexpr int kRows = 128, kPanel = 128 * 128; // rows of a tile, bytes of a panel of 64 columns
 constexpr int kFwdThreads = 384;
 // launched with 168 registers a thread (64512 of a block): 2 x 128 x 208 + 128 x 88 = 64512
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
@@ -39,28 +37,6 @@ struct FwdBarriers {
   unsigned tmem;
   volatile unsigned abort;
 };
-
-// Slot -> sequence and block of 256 rows.  Sequence b's blocks start at slot cu[b] / 256 + b: there is room for each
-// sequence's last, partial block, and no prefix sum is needed; slots in between are empty.  Sequence number
-// `sequences` stands for the rows behind the last one.
-struct Place {
-  int first, end, block;
-};
-__device__ __forceinline__ Place place_of(const AttnArgs &a, int slot, int rows) {
-  auto start = [&](int b) { return min(max(b < 0 ? 0 : a.cu[b], 0), a.tokens); };
-  int lo = 0, hi = a.sequences;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (start(mid) / rows + mid <= slot) lo = mid;
-    else hi = mid - 1;
-  }
-  Place p;
-  p.first = start(lo);
-  p.end = lo == a.sequences ? a.tokens : start(lo + 1);
-  p.block = slot - (p.first / rows + lo);
-  if (lo == a.sequences) p.block = -1 - p.block; // no sequence: encoded as a negative block
-  return p;
-}
 
 template <int HD>
 __global__ void __launch_bounds__(kFwdThreads, 1)
@@ -110,44 +86,32 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         int issued = 0; // K and V tiles in flight or landed, for the give-up path
         mbar_expect_tx(&bar.q_full, (two ? 2 : 1) * L::kTileBytes);
         for (int w = 0; w < (two ? 2 : 1); ++w)
-          for (int p = 0; p < L::kPanels; ++p) load_panel(smem + L::kQ + w * L::kTileBytes + p * kPanel, mq, p * 64, h, q0 + w * kRows, &bar.q_full);
+          load_tile<HD>(smem + L::kQ + w * L::kTileBytes, mq, h, q0 + w * kRows, &bar.q_full);
         for (int it = 0; it < tiles; ++it) {
           const int s = it % L::kStages, row = at.first + (tiles - 1 - it) * kRows;
           const unsigned ph = ((it / L::kStages) & 1) ^ 1;
           if (!wait_or_abort(&bar.k_empty[s], ph, &bar.abort)) break;
           mbar_expect_tx(&bar.k_full[s], L::kTileBytes);
-          for (int p = 0; p < L::kPanels; ++p) load_panel(smem + L::kK + s * L::kTileBytes + p * kPanel, mk, p * 64, g, row, &bar.k_full[s]);
+          load_tile<HD>(smem + L::kK + s * L::kTileBytes, mk, g, row, &bar.k_full[s]);
           issued = 2 * it + 1;
           if (!wait_or_abort(&bar.v_empty[s], ph, &bar.abort)) break;
           mbar_expect_tx(&bar.v_full[s], L::kTileBytes);
-          for (int p = 0; p < L::kPanels; ++p) load_panel(smem + L::kV + s * L::kTileBytes + p * kPanel, mv, p * 64, g, row, &bar.v_full[s]);
+          load_tile<HD>(smem + L::kV + s * L::kTileBytes, mv, g, row, &bar.v_full[s]);
           issued = 2 * it + 2;
         }
-        // shared memory is not given back under a copy: those still in flight are waited for, within a limit
-        if (issued < 2 * tiles) {
-          mbar_wait_bounded(&bar.q_full, 0, kOpWaitNs, nullptr);
-          for (int n = issued - 1; n >= 0 && n >= issued - 2 * L::kStages; --n) {
-            const int it = n / 2, s = it % L::kStages;
-            mbar_wait_bounded(n & 1 ? &bar.v_full[s] : &bar.k_full[s], (it / L::kStages) & 1, kOpWaitNs, nullptr);
-          }
-        }
+        if (issued < 2 * tiles) land_copies<L::kStages>(issued, &bar.q_full, bar.k_full, bar.v_full);
       }
     } else if (warp == 8) {
       // --------------------------------------------------------------------- matrix products
       if (lane == 0) {
         const unsigned qk_desc = mma_desc(128, false, false) | (negate ? 1u << 13 : 0u), pv_desc = mma_desc(HD, false, true);
         auto qk = [&](int w, int s) {
-          const unsigned q = smem + L::kQ + w * L::kTileBytes, k = smem + L::kK + s * L::kTileBytes;
-  #pragma unroll
-          for (int i = 0; i < HD / 16; ++i) {
-            const unsigned off = (i / 4) * kPanel + (i % 4) * 32;
-            mma_ss(tmem + w * 128, tile_desc(q + off, kPanel), tile_desc(k + off, kPanel), qk_desc, i > 0);
-          }
+          product_ss<HD>(tmem + w * 128, smem + L::kQ + w * L::kTileBytes, smem + L::kK + s * L::kTileBytes, qk_desc);
           mma_commit(&bar.s_full[w]);
         };
         auto pv = [&](int w, int s, bool add) {
           const unsigned v = smem + L::kV + s * L::kTileBytes;
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < 8; ++i)
             mma_ts(tmem + 256 + w * HD, tmem + w * 128 + i * 8, tile_desc(v + i * 2048, kPanel), pv_desc, add || i > 0);
         };
@@ -258,13 +222,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
           if (valid < kRows) {
             ok = warp_wait(&bar.v_full[0], 0, &bar.abort);
             if (!ok) break;
-            if (r >= valid) {
-#pragma unroll
-              for (int p = 0; p < L::kPanels; ++p)
-#pragma unroll
-                for (int u = 0; u < 8; ++u)
-                  asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(smem + L::kV + p * kPanel + r * 128 + u * 16), "r"(0) : "memory");
-            }
+            if (r >= valid) zero_row<HD>(smem + L::kV, r, 0), zero_row<HD>(smem + L::kV, r, 1);
             fence_async_smem();
           }
         }

@@ -133,19 +133,4 @@ __device__ __forceinline__ void attn_dkv_row(const AttnArgs &a, int j, int g, in
     }
 }
 
-// The sequence of token i: its first row and one past its last; first = -1: the row belongs to none.  Whatever
-// cu_seqlens holds, 0 <= first <= i < end <= tokens where first >= 0.
-__device__ __forceinline__ void sequence_of(const AttnArgs &a, int i, int &first, int &end) {
-  int lo = 0, hi = a.sequences - 1; // the last sequence that starts at or before i
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.cu[mid] <= i) lo = mid;
-    else hi = mid - 1;
-  }
-  first = -1, end = -1;
-  if (a.sequences == 0) return;
-  const int s = max(a.cu[lo], 0), e = min(a.cu[lo + 1], a.tokens);
-  if (s <= i && i < e) first = s, end = e;
-}
-
 } // namespace diloco
