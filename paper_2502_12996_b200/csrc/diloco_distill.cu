@@ -7,11 +7,12 @@
 //
 // A row of logits is read once and its gradient written once; memory bounds it as long as a row is not read
 // twice, so one block holds a whole row in registers (16-byte accesses, RV of them a thread): maximum, sum of
-// exponentials and gradient all come from that copy.  Rows that fit no block are read twice, the second time
-// mostly from L2.  Rows need not start on 16 bytes (an odd vocabulary): the elements before the first and
-// after the last whole access are taken one by one.  The teacher's few entries are fetched while the row's
-// loads are in flight; where they touch the gradient, the thread that owns the first entry of an id writes
-// that element again after the row, with the sum of all entries of the id, so nothing is added by atomics.
+// exponentials and gradient all come from that copy, while the next row is already on its way to shared memory.
+// One warp of the block has the teacher's entries and nothing else: their fetch, softmax and share of the loss, and the
+// elements of the gradient that they touch, are as long a chain of small steps as the row itself.  Rows that fit no
+// block are read twice, the second time mostly from L2.  Rows need not start on 16 bytes (an odd vocabulary): the
+// elements before the first and after the last whole access are taken one by one.  An element that several entries
+// point at is written once, with the sum of their shares, so nothing is added by atomics.
 #include <type_traits>
 
 #include "diloco_ops.cuh"
@@ -31,14 +32,15 @@ struct DistillArgs {
   float temperature, inv_t, z, grad_scale;
 };
 
-// The teacher's side of one row in shared memory.
+// The teacher's side of one row in shared memory, k entries each.
 constexpr int kMaxK = 1024;
 struct Teacher {
-  int id[kMaxK];   // -1: unused
-  float p[kMaxK];  // t / T, then the share of the entry
-  float x[kMaxK];  // the student's logit there
-  float red[3][32];
+  int *id;      // -1: unused
+  float *p, *x; // t / T, then the share of the entry; the student's logit there
+  __device__ __forceinline__ Teacher(unsigned char *at, int k)
+      : id(reinterpret_cast<int *>(at)), p(reinterpret_cast<float *>(at) + k), x(reinterpret_cast<float *>(at) + 2 * k) {}
 };
+constexpr int teacher_bytes(int k) { return 12 * k; }
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -51,31 +53,32 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Entries of row n into shared memory (any number of threads); the caller synchronises.
-template <typename T> __device__ __forceinline__ void fetch_teacher(const DistillArgs &a, long long n, const T *row, Teacher &t) {
-  for (int i = threadIdx.x; i < a.k; i += blockDim.x) {
-    const long long at = n * a.k + i;
-    const long long id = a.ids64 ? static_cast<const long long *>(a.ids)[at] : (long long)static_cast<const int *>(a.ids)[at];
-    const bool used = id >= 0 && id < a.vocab;
-    t.id[i] = used ? (int)id : -1;
-    float x[1] = {0.f}, q = 0.f;
-    if (used) {
-      load_vec<T, 1>(row + id, x);
-      q = a.teacher_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(a.teacher)[at]) : static_cast<const float *>(a.teacher)[at];
-    }
-    t.x[i] = x[0];
-    t.p[i] = q * a.inv_t;
-  }
+// Entries of a row by one warp, 32 at a time.
+__device__ __forceinline__ int entry_id(const DistillArgs &a, long long n, int i) {
+  const long long at = n * a.k + i;
+  const long long id = a.ids64 ? static_cast<const long long *>(a.ids)[at] : (long long)static_cast<const int *>(a.ids)[at];
+  return id >= 0 && id < a.vocab ? (int)id : -1;
 }
-
-// One warp: t.p becomes the softmax over the used entries; returns sum_k p_k (log p_k - x_k / T), and in `any`
-// whether an entry is used.
-__device__ __forceinline__ float finish_teacher(const DistillArgs &a, Teacher &t, bool &any) {
+__device__ __forceinline__ float entry_logit(const DistillArgs &a, long long n, int i) {
+  const long long at = n * a.k + i;
+  return (a.teacher_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(a.teacher)[at]) : static_cast<const float *>(a.teacher)[at]) * a.inv_t;
+}
+// Everything of row n's teacher that does not need the row's log-sum-exp: t.x, and t.p as the softmax over the used
+// entries.  Returns sum_k p_k (log p_k - x_k / T), and in `any` whether an entry is used.
+template <typename T> __device__ __forceinline__ float read_teacher(const DistillArgs &a, Teacher t, long long n, const T *row, bool &any) {
   const int lane = threadIdx.x & 31;
   float top = -INFINITY, total = 0.f, kl = 0.f;
   bool mine = false;
-  for (int i = lane; i < a.k; i += 32)
-    if (t.id[i] >= 0) top = fmaxf(top, t.p[i]), mine = true;
+  for (int i = lane; i < a.k; i += 32) {
+    const int id = entry_id(a, n, i);
+    float x[1] = {0.f};
+    if (id >= 0) load_vec<T, 1>(row + id, x);
+    const float q = entry_logit(a, n, i);
+    t.id[i] = id;
+    t.p[i] = q;
+    t.x[i] = x[0];
+    if (id >= 0) top = fmaxf(top, q), mine = true;
+  }
   any = __any_sync(0xffffffffu, mine);
   top = warp_max(top);
   for (int i = lane; i < a.k; i += 32)
@@ -91,13 +94,32 @@ __device__ __forceinline__ float finish_teacher(const DistillArgs &a, Teacher &t
     }
     t.p[i] = p;
   }
+  __syncwarp();
   return warp_sum(kl);
 }
 
-// After the row's gradient: elements that teacher entries point at, each by the thread of its first entry.
-template <typename T>
-__device__ __forceinline__ void put_teacher(const DistillArgs &a, const Teacher &t, T *grad, float lse2, float coef, float wt) {
-  for (int i = threadIdx.x; i < a.k; i += blockDim.x) {
+// What a row's loss and gradient need once its log-sum-exp is known: dx = 2^(x log2(e) / T - lse2) coef, less wt p.
+struct RowScale {
+  float lse, lse2, coef, wt;
+};
+__device__ __forceinline__ RowScale row_scale(const DistillArgs &a, float m, float s, float wn, bool any) {
+  RowScale r;
+  r.lse2 = m + log2f(s);
+  r.lse = r.lse2 * kLn2;
+  r.wt = any ? wn * a.temperature : 0.f;
+  r.coef = any ? wn * (a.temperature + 2.f * a.z * r.lse * a.inv_t) : 0.f;
+  return r;
+}
+__device__ __forceinline__ float term(float x, float c, const RowScale &r) { return ex2(fmaf(x, c, -r.lse2)) * r.coef; }
+__device__ __forceinline__ void put_loss(const DistillArgs &a, long long n, const RowScale &r, float kl, float wn, bool any) {
+  if ((threadIdx.x & 31) == 0) {
+    a.loss[n] = any ? wn * (a.temperature * a.temperature * (kl + r.lse) + a.z * r.lse * r.lse) : 0.f;
+    a.lse[n] = r.lse;
+  }
+}
+// After the row's gradient, by the teacher's warp: elements that its entries point at, each by its first entry.
+template <typename T> __device__ __forceinline__ void put_teacher(const DistillArgs &a, Teacher t, T *grad, const RowScale &r) {
+  for (int i = threadIdx.x & 31; i < a.k; i += 32) {
     const int id = t.id[i];
     if (id < 0) continue;
     bool first = true;
@@ -108,7 +130,7 @@ __device__ __forceinline__ void put_teacher(const DistillArgs &a, const Teacher 
         p += t.p[j];
       }
     if (!first) continue;
-    const float g[1] = {ex2(fmaf(t.x[i], a.inv_t * kLog2e, -lse2)) * coef - wt * p};
+    const float g[1] = {term(t.x[i], a.inv_t * kLog2e, r) - r.wt * p};
     store_vec<T, 1>(grad + id, g);
   }
 }
@@ -127,107 +149,184 @@ template <typename T, int W> __device__ __forceinline__ Span span_of(const T *ro
   return s;
 }
 
-// Combines the threads' (max, sum) pairs of base-2 exponentials; every thread gets both.
-template <int NT> __device__ __forceinline__ void block_lse(float &m, float &s, float (*red)[32]) {
+// Barriers of a block whose warps come to them at different places of the program: plain ones by number.  (A reducing
+// barrier such as __syncthreads_or has to be one and the same instruction for the whole block.)
+template <int ID, int NT> __device__ __forceinline__ void block_sync() { asm volatile("barrier.cta.sync %0, %1;" ::"n"(ID), "n"(NT) : "memory"); }
+
+// What the warps of a row leave for each other before the first barrier.
+struct Partial {
+  float m[32], s[32];
+  int any;
+};
+__device__ __forceinline__ void put_partial(Partial &red, float m, float s) {
   const float wm = warp_max(m);
   s = wm == -INFINITY ? s : s * ex2(m - wm); // m = -inf: s is 0
   s = warp_sum(s);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (lane == 0) red[0][warp] = wm, red[1][warp] = s;
-  __syncthreads();
-  float bm = lane < NT / 32 ? red[0][lane] : -INFINITY, bs = lane < NT / 32 ? red[1][lane] : 0.f;
-  const float top = warp_max(bm);
-  bs = bm == -INFINITY ? 0.f : bs * ex2(bm - top);
-  s = warp_sum(bs);
-  m = top;
+  if ((threadIdx.x & 31) == 0) red.m[threadIdx.x >> 5] = wm, red.s[threadIdx.x >> 5] = s;
+}
+// After the barrier: maximum and sum of base-2 exponentials over `warps` warps, in every thread.
+__device__ __forceinline__ void get_partial(const Partial &red, int warps, float &m, float &s) {
+  const int lane = threadIdx.x & 31;
+  const float bm = lane < warps ? red.m[lane] : -INFINITY, bs = lane < warps ? red.s[lane] : 0.f;
+  m = warp_max(bm);
+  s = warp_sum(bm == -INFINITY ? bs : bs * ex2(bm - m)); // bm = -inf: bs is 0, or NaN
 }
 
-template <typename T, int W, int NT, int RV>
-__global__ void __launch_bounds__(NT, 1) distill_resident_kernel(const DistillArgs a) {
-  using Raw = typename Pack<T, W>::raw;
-  __shared__ Teacher t;
-  const float c = a.inv_t * kLog2e;
-  for (long long n = blockIdx.x; n < a.rows; n += gridDim.x) {
-    const T *row = static_cast<const T *>(a.logits) + n * a.logits_stride;
-    const Span sp = span_of<T, W>(row, a.vocab);
-    const T *body = row + sp.head;
-    Raw raw[RV];
+__device__ __forceinline__ void copy_async16(unsigned smem, const void *g) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(g) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+
+// The largest of an access's elements
+__device__ __forceinline__ float pack_max(const float4 &r) { return fmaxf(fmaxf(r.x, r.y), fmaxf(r.z, r.w)); }
+__device__ __forceinline__ float pack_max(const uint4 &r) {
+  const __nv_bfloat162 m = __hmax2(__hmax2(reinterpret_cast<const __nv_bfloat162 &>(r.x), reinterpret_cast<const __nv_bfloat162 &>(r.y)),
+                                   __hmax2(reinterpret_cast<const __nv_bfloat162 &>(r.z), reinterpret_cast<const __nv_bfloat162 &>(r.w)));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+
+// An access's elements: sum of 2^(x c - m0), and 2^(x c - lse2) coef
+__device__ __forceinline__ void add_terms(const float4 &r, float2 c, float2 m0, float2 &s) {
+  const float2 u = fma2(make_float2(r.x, r.y), c, m0), v = fma2(make_float2(r.z, r.w), c, m0);
+  s = add2(s, add2(make_float2(ex2(u.x), ex2(u.y)), make_float2(ex2(v.x), ex2(v.y))));
+}
+__device__ __forceinline__ void add_terms(const uint4 &r, float2 c, float2 m0, float2 &s) {
+  const unsigned w[4] = {r.x, r.y, r.z, r.w};
+  float2 t[4];
 #pragma unroll
-    for (int i = 0; i < RV; ++i) {
-      const int v = i * NT + threadIdx.x;
-      if (v < sp.body) raw[i] = reinterpret_cast<const Raw *>(body)[v];
+  for (int i = 0; i < 4; ++i) {
+    const float2 u = fma2(make_float2(bf16_lo(w[i]), bf16_hi(w[i])), c, m0);
+    t[i] = make_float2(ex2(u.x), ex2(u.y));
+  }
+  s = add2(s, add2(add2(t[0], t[1]), add2(t[2], t[3])));
+}
+__device__ __forceinline__ float4 terms(const float4 &r, float2 c, float2 lse2, float2 coef) {
+  float2 u = fma2(make_float2(r.x, r.y), c, lse2), v = fma2(make_float2(r.z, r.w), c, lse2);
+  u = mul2(make_float2(ex2(u.x), ex2(u.y)), coef), v = mul2(make_float2(ex2(v.x), ex2(v.y)), coef);
+  return make_float4(u.x, u.y, v.x, v.y);
+}
+__device__ __forceinline__ uint4 terms(const uint4 &r, float2 c, float2 lse2, float2 coef) {
+  const unsigned w[4] = {r.x, r.y, r.z, r.w};
+  unsigned o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float2 u = fma2(make_float2(bf16_lo(w[i]), bf16_hi(w[i])), c, lse2);
+    u = mul2(make_float2(ex2(u.x), ex2(u.y)), coef);
+    o[i] = bf16_pair(u.x, u.y);
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// Rows of at most (NT - 32) * RV accesses: NT - 32 threads for the row, the last warp for the teacher.  The next row is
+// on its way into shared memory (each thread copies what it will itself read, so no barrier is needed) while this
+// one is worked on.  Two barriers a row: sums and teacher are known; the row's gradient is written.
+template <typename T, int NT, int RV>
+__global__ void __launch_bounds__(NT, 512 / NT) distill_resident_kernel(const DistillArgs a) {
+  constexpr int W = 16 / (int)sizeof(T), NC = NT - 32;
+  using Raw = typename Pack<T, W>::raw;
+  extern __shared__ __align__(16) unsigned char staged[]; // [RV][NC] accesses, then the teacher
+  __shared__ Partial red;
+  const int tid = threadIdx.x;
+  const float c = a.inv_t * kLog2e;
+  auto row_of = [&](long long n) { return static_cast<const T *>(a.logits) + n * a.logits_stride; };
+  auto weight_of = [&](long long n) { return a.grad_scale * (a.row_weight ? a.row_weight[n] : 1.f); };
+  if (tid >= NC) {
+    const Teacher t(staged + NC * RV * 16, a.k);
+    for (long long n = blockIdx.x; n < a.rows; n += gridDim.x) {
+      bool any;
+      const float kl = read_teacher<T>(a, t, n, row_of(n), any);
+      const float wn = weight_of(n);
+      if (tid == NC) red.any = any;
+      block_sync<1, NT>();
+      float m, s;
+      get_partial(red, NC / 32, m, s);
+      const RowScale r = row_scale(a, m, s, wn, any);
+      put_loss(a, n, r, kl, wn, any);
+      block_sync<2, NT>();
+      if (a.dlogits && any) put_teacher<T>(a, t, static_cast<T *>(a.dlogits) + n * a.grad_stride, r);
+      __syncwarp();
     }
-    // one single element for each of the first head + tail threads
-    const int odd = (int)threadIdx.x < sp.head ? (int)threadIdx.x
-                    : (int)threadIdx.x < sp.head + sp.tail ? sp.body * W + (int)threadIdx.x : -1;
-    float single[1] = {-INFINITY};
-    if (odd >= 0) load_vec<T, 1>(row + odd, single);
-    fetch_teacher<T>(a, n, row, t);
-    float m = single[0];
+    return;
+  }
+  const Raw *mine = reinterpret_cast<const Raw *>(staged) + tid;
+  const unsigned to = (unsigned)__cvta_generic_to_shared(staged) + tid * 16;
+  // the single elements before and after a row's whole accesses: one for each of the first head + tail threads
+  auto odd_of = [&](const Span &sp) { return tid < sp.head ? tid : tid < sp.head + sp.tail ? sp.body * W + tid : -1; };
+  auto fetch = [&](const T *row, const Span &sp) {
 #pragma unroll
     for (int i = 0; i < RV; ++i)
-      if (i * NT + (int)threadIdx.x < sp.body) {
-        float v[W];
-        unpack(raw[i], v);
+      if (i * NC + tid < sp.body) copy_async16(to + i * NC * 16, row + sp.head + (long long)(i * NC + tid) * W);
+    copy_commit();
+  };
+  long long n = blockIdx.x;
+  if (n >= a.rows) return;
+  Span sp = span_of<T, W>(row_of(n), a.vocab);
+  fetch(row_of(n), sp);
+  int odd = odd_of(sp);
+  float single[1] = {-INFINITY};
+  if (odd >= 0) load_vec<T, 1>(row_of(n) + odd, single);
+  while (n < a.rows) {
+    const long long next = n + gridDim.x;
+    const float wn = weight_of(n), one = single[0];
+    const int at = odd;
+    copy_wait();
+    Raw raw[RV];
+    float m = one;
 #pragma unroll
-        for (int j = 0; j < W; ++j) m = fmaxf(m, v[j]);
+    for (int i = 0; i < RV; ++i)
+      if (i * NC + tid < sp.body) {
+        raw[i] = mine[i * NC];
+        m = fmaxf(m, pack_max(raw[i]));
       }
+    // every staged element is in a register: the next row may land in its place
+    const int head = sp.head, body = sp.body;
+    single[0] = -INFINITY;
+    if (next < a.rows) {
+      sp = span_of<T, W>(row_of(next), a.vocab);
+      fetch(row_of(next), sp);
+      odd = odd_of(sp);
+      if (odd >= 0) load_vec<T, 1>(row_of(next) + odd, single);
+    }
     m *= c;
     const float m0 = m == -INFINITY ? 0.f : m; // nothing but -infinity (or no element): every term is 0
-    float s = odd >= 0 ? ex2(fmaf(single[0], c, -m0)) : 0.f;
+    const float2 cc = make_float2(c, c), mm = make_float2(-m0, -m0);
+    float2 two = make_float2(at >= 0 ? ex2(fmaf(one, c, -m0)) : 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < RV; ++i)
-      if (i * NT + (int)threadIdx.x < sp.body) {
-        float v[W];
-        unpack(raw[i], v);
-#pragma unroll
-        for (int j = 0; j < W; ++j) s += ex2(fmaf(v[j], c, -m0));
-      }
-    block_lse<NT>(m, s, t.red); // its barrier also ends the fetch of the teacher's entries
-    const float lse2 = m + log2f(s), lse = lse2 * kLn2;
-    const float wn = a.grad_scale * (a.row_weight ? a.row_weight[n] : 1.f);
-    if (threadIdx.x < 32) {
-      bool any;
-      const float kl = finish_teacher(a, t, any);
-      if (threadIdx.x == 0) {
-        a.loss[n] = any ? wn * (a.temperature * a.temperature * (kl + lse) + a.z * lse * lse) : 0.f;
-        a.lse[n] = lse;
-        t.red[2][0] = any ? 1.f : 0.f;
-      }
-    }
+      if (i * NC + tid < body) add_terms(raw[i], cc, mm, two);
+    put_partial(red, m, two.x + two.y);
+    block_sync<1, NT>();
     if (a.dlogits) {
-      __syncthreads();
-      const float wt = t.red[2][0] != 0.f ? wn * a.temperature : 0.f;
-      const float coef = t.red[2][0] != 0.f ? wn * (a.temperature + 2.f * a.z * lse * a.inv_t) : 0.f;
+      float s;
+      get_partial(red, NC / 32, m, s);
+      const bool any = red.any != 0;
+      const RowScale r = row_scale(a, m, s, wn, any);
       T *grad = static_cast<T *>(a.dlogits) + n * a.grad_stride;
+      const float2 lse2 = make_float2(-r.lse2, -r.lse2), coef = make_float2(r.coef, r.coef);
+      Raw *out = reinterpret_cast<Raw *>(grad + head) + tid;
 #pragma unroll
-      for (int i = 0; i < RV; ++i) {
-        const int v = i * NT + threadIdx.x;
-        if (v < sp.body) {
-          float x[W];
-          unpack(raw[i], x);
-#pragma unroll
-          for (int j = 0; j < W; ++j) x[j] = ex2(fmaf(x[j], c, -lse2)) * coef;
-          store_vec<T, W>(grad + sp.head + (long long)v * W, x);
-        }
+      for (int i = 0; i < RV; ++i)
+        if (i * NC + tid < body) out[i * NC] = terms(raw[i], cc, lse2, coef);
+      if (at >= 0) {
+        const float x[1] = {term(one, c, r)};
+        store_vec<T, 1>(grad + at, x);
       }
-      if (odd >= 0) {
-        single[0] = ex2(fmaf(single[0], c, -lse2)) * coef;
-        store_vec<T, 1>(grad + odd, single);
-      }
-      __syncthreads(); // the row is written before single elements of it are written again
-      if (wt != 0.f) put_teacher<T>(a, t, grad, lse2, coef, wt);
     }
-    __syncthreads(); // the next row's entries
+    block_sync<2, NT>(); // the row is written, `red` is read
+    n = next;
   }
 }
 
-// Rows that no block holds: two passes over memory.
+// Rows that no block holds, or whose gradient starts at another place within 16 bytes (W = 1): two passes over memory.
 constexpr int kStreamThreads = 512;
-template <typename T, int W> __global__ void __launch_bounds__(kStreamThreads) distill_stream_kernel(const DistillArgs a) {
+template <typename T, int W> __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const DistillArgs a) {
   using Raw = typename Pack<T, W>::raw;
-  __shared__ Teacher t;
+  extern __shared__ __align__(16) unsigned char staged[];
+  const Teacher t(staged, a.k);
+  __shared__ Partial red;
   const float c = a.inv_t * kLog2e;
+  const bool teacher = threadIdx.x >= kStreamThreads - 32;
   for (long long n = blockIdx.x; n < a.rows; n += gridDim.x) {
     const T *row = static_cast<const T *>(a.logits) + n * a.logits_stride;
     const Span sp = span_of<T, W>(row, a.vocab);
@@ -236,7 +335,9 @@ template <typename T, int W> __global__ void __launch_bounds__(kStreamThreads) d
                     : (int)threadIdx.x < sp.head + sp.tail ? sp.body * W + (int)threadIdx.x : -1;
     float single[1] = {-INFINITY};
     if (odd >= 0) load_vec<T, 1>(row + odd, single);
-    fetch_teacher<T>(a, n, row, t);
+    bool used = false;
+    float kl = 0.f;
+    if (teacher) kl = read_teacher<T>(a, t, n, row, used);
     float m = single[0] * c, s = odd >= 0 ? 1.f : 0.f;
     if (m == -INFINITY) s = 0.f; // exp(-inf) counts nothing
 #pragma unroll 4
@@ -255,39 +356,32 @@ template <typename T, int W> __global__ void __launch_bounds__(kStreamThreads) d
 #pragma unroll
       for (int j = 0; j < W; ++j) s += v[j] == -INFINITY ? 0.f : ex2(v[j] - m);
     }
-    block_lse<kStreamThreads>(m, s, t.red);
-    const float lse2 = m + log2f(s), lse = lse2 * kLn2;
+    put_partial(red, m, s);
+    if (threadIdx.x == kStreamThreads - 32) red.any = used;
+    __syncthreads();
+    get_partial(red, kStreamThreads / 32, m, s);
+    const bool any = red.any != 0;
     const float wn = a.grad_scale * (a.row_weight ? a.row_weight[n] : 1.f);
-    if (threadIdx.x < 32) {
-      bool any;
-      const float kl = finish_teacher(a, t, any);
-      if (threadIdx.x == 0) {
-        a.loss[n] = any ? wn * (a.temperature * a.temperature * (kl + lse) + a.z * lse * lse) : 0.f;
-        a.lse[n] = lse;
-        t.red[2][0] = any ? 1.f : 0.f;
-      }
-    }
+    const RowScale r = row_scale(a, m, s, wn, any);
+    if (teacher) put_loss(a, n, r, kl, wn, any);
+    T *grad = static_cast<T *>(a.dlogits) + n * a.grad_stride;
     if (a.dlogits) {
-      __syncthreads();
-      const float wt = t.red[2][0] != 0.f ? wn * a.temperature : 0.f;
-      const float coef = t.red[2][0] != 0.f ? wn * (a.temperature + 2.f * a.z * lse * a.inv_t) : 0.f;
-      T *grad = static_cast<T *>(a.dlogits) + n * a.grad_stride;
 #pragma unroll 4
       for (int i = threadIdx.x; i < sp.body; i += kStreamThreads) {
         float x[W];
         unpack(body[i], x);
 #pragma unroll
-        for (int j = 0; j < W; ++j) x[j] = ex2(fmaf(x[j], c, -lse2)) * coef;
+        for (int j = 0; j < W; ++j) x[j] = term(x[j], c, r);
         store_vec<T, W>(grad + sp.head + (long long)i * W, x);
       }
       if (odd >= 0) {
-        single[0] = ex2(fmaf(single[0], c, -lse2)) * coef;
+        single[0] = term(single[0], c, r);
         store_vec<T, 1>(grad + odd, single);
       }
-      __syncthreads();
-      if (wt != 0.f) put_teacher<T>(a, t, grad, lse2, coef, wt);
     }
-    __syncthreads();
+    __syncthreads(); // the row is written, `red` is read
+    if (teacher && a.dlogits && any) put_teacher<T>(a, t, grad, r);
+    __syncwarp();
   }
 }
 
@@ -301,23 +395,36 @@ int valid(const diloco_distill_t *l) {
   return DILOCO_OK;
 }
 
-template <typename T, int W> void launch(const DistillArgs &a, int sms, cudaStream_t s) {
-  const long long n = (a.vocab + W - 1) / W;
-  auto grid = [&](int per_sm) { return (unsigned)(a.rows < (long long)sms * per_sm ? a.rows : (long long)sms * per_sm); };
-  if (n <= 256) distill_resident_kernel<T, W, 128, 2><<<grid(8), 128, 0, s>>>(a);
-  else if (n <= 1024) distill_resident_kernel<T, W, 256, 4><<<grid(4), 256, 0, s>>>(a);
-  else if (n <= 4096) distill_resident_kernel<T, W, 512, 8><<<grid(2), 512, 0, s>>>(a);
-  else if (n <= 8192) distill_resident_kernel<T, W, 1024, 8><<<grid(1), 1024, 0, s>>>(a);
-  else distill_stream_kernel<T, W><<<grid(4), kStreamThreads, 0, s>>>(a);
+constexpr int kHeld = 18; // accesses a thread holds: 72 registers of 128
+template <typename T, int NT> int launch_resident(const DistillArgs &a, int sms, cudaStream_t s) {
+  constexpr int kRow = (NT - 32) * kHeld * 16;
+  const int bytes = kRow + teacher_bytes(a.k);
+  static const bool ok = cudaFuncSetAttribute(distill_resident_kernel<T, NT, kHeld>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              kRow + teacher_bytes(kMaxK)) == cudaSuccess;
+  if (!ok) return cuda_fail(cudaGetLastError());
+  // 128 registers a thread and this shared memory: blocks that an SM holds
+  const int by_smem = (227 * 1024) / (bytes + 2048), per_sm = by_smem < 512 / NT ? by_smem : 512 / NT;
+  const long long most = (long long)sms * (per_sm < 1 ? 1 : per_sm);
+  distill_resident_kernel<T, NT, kHeld><<<(unsigned)(a.rows < most ? a.rows : most), NT, bytes, s>>>(a);
+  return launched();
+}
+template <typename T, int W> int launch_stream(const DistillArgs &a, int sms, cudaStream_t s) {
+  distill_stream_kernel<T, W><<<(unsigned)(a.rows < sms * 4ll ? a.rows : sms * 4ll), kStreamThreads, teacher_bytes(a.k), s>>>(a);
+  return launched();
 }
 
-template <typename T> void launch_any(const DistillArgs &a, int sms, cudaStream_t s) {
+template <typename T> int launch_any(const DistillArgs &a, int sms, cudaStream_t s) {
   constexpr int W = 16 / (int)sizeof(T);
   // whole accesses need the same place within 16 bytes in a row of logits and in its gradient
   const auto x = reinterpret_cast<uintptr_t>(a.logits), g = reinterpret_cast<uintptr_t>(a.dlogits);
   const bool same = !a.dlogits || ((x - g) % 16 == 0 && ((a.logits_stride - a.grad_stride) * (long long)sizeof(T)) % 16 == 0);
-  if (same) launch<T, W>(a, sms, s);
-  else distill_stream_kernel<T, 1><<<(unsigned)(a.rows < sms * 4ll ? a.rows : sms * 4ll), kStreamThreads, 0, s>>>(a);
+  if (!same) return launch_stream<T, 1>(a, sms, s);
+  const long long n = (a.vocab + W - 1) / W; // accesses of a row
+  if (n <= 32 * kHeld) return launch_resident<T, 64>(a, sms, s);
+  if (n <= 96 * kHeld) return launch_resident<T, 128>(a, sms, s);
+  if (n <= 224 * kHeld) return launch_resident<T, 256>(a, sms, s);
+  if (n <= 480 * kHeld) return launch_resident<T, 512>(a, sms, s);
+  return launch_stream<T, W>(a, sms, s);
 }
 
 } // namespace
@@ -342,7 +449,6 @@ extern "C" int diloco_distill_loss(const diloco_distill_t *l, const void *logits
   a.k = l->k, a.ids64 = l->ids_int64, a.teacher_bf16 = l->teacher_dtype == DILOCO_DTYPE_BF16;
   a.temperature = l->temperature, a.inv_t = 1.f / l->temperature, a.z = l->z_coef, a.grad_scale = l->grad_scale;
   const int sms = sm_count(pc.device);
-  if (l->dtype == DILOCO_DTYPE_F32) launch_any<float>(a, sms, static_cast<cudaStream_t>(stream));
-  else launch_any<__nv_bfloat16>(a, sms, static_cast<cudaStream_t>(stream));
-  return launched();
+  return l->dtype == DILOCO_DTYPE_F32 ? launch_any<float>(a, sms, static_cast<cudaStream_t>(stream))
+                                      : launch_any<__nv_bfloat16>(a, sms, static_cast<cudaStream_t>(stream));
 }

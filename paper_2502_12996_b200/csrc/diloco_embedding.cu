@@ -8,11 +8,12 @@
 // holds its sum, with no atomics on values.  Four launches, each one's start overlapping the end of the last:
 //   1 tiles    2048 tokens a block: stable partition by the id's low 8 bits (text uses low ids most, so low
 //              bits spread them: the top token of a 1/rank law is 7 % of the tokens, not half of a bucket)
-//   2 buckets  a block for each of the 256: gathers its pieces of all tiles in tile order, counts its ids, and
-//              places its tokens stably by id (every id belongs to one warp, which reads in order)
+//   2 buckets  a block for each of the 256: gathers its pieces of all tiles in tile order, counts its ids,
+//              places its tokens stably by id (every id belongs to one warp, which reads in order), and zeroes the
+//              rows of ids that no token has: the stores fill the memory system while other blocks sort
 //   3 sums     the sorted tokens in chunks of C, whatever ids they hold (an even split for any distribution): rows
 //              are added in order in registers; a run of one id inside a chunk is finished and written, a run
-//              that crosses chunks leaves fp32 partial sums.  The same launch zeroes the rows of absent ids.
+//              that crosses chunks leaves fp32 partial sums
 //   4 join     runs that cross chunks: partial sums in chunk order, written by the chunk where the run starts
 // Sums run in token order inside a chunk, then in chunk order: a fixed order for given ids.
 #include <type_traits>
@@ -32,6 +33,7 @@ struct EmbedArgs {
   void *out, *dtable;
   long long tokens, vocab, table_stride, grad_stride, row_stride;
   int M, d, ids64, accumulate;
+  int grad_bytes; // of an element of dtable
   float scale;
   // workspace of the backward, all [M, ...]
   uint2 *tile_sorted, *gathered, *sorted; // [tokens] {id, token}: tile by tile, bucket by bucket, in order
@@ -47,35 +49,40 @@ __device__ __forceinline__ long long id_at(const EmbedArgs &a, long long i) {
 }
 
 // ---------------------------------------------------------------------------------- forward
+// A worker (`lanes` threads) takes ROWS tokens at a time, so that as many rows are in flight at once, and reads the
+// next ones' ids before it waits for these rows.  Blocks stay (8 on an SM): with a block for every 2 rows each, the
+// wait for the ids was not hidden and 65536 rows of 4 KB took 100 us.
 template <typename TT, typename AT, int VW, int ROWS>
 __global__ void __launch_bounds__(kWorkThreads) embed_forward_kernel(const EmbedArgs a, int lanes) {
-  const int lane = threadIdx.x % lanes;
-  const long long n = a.tokens * a.M;
-  const long long r0 = ((long long)blockIdx.x * (kWorkThreads / lanes) + threadIdx.x / lanes) * ROWS;
-  long long src[ROWS];
+  const int lane = threadIdx.x % lanes, workers = kWorkThreads / lanes;
+  const long long n = a.tokens * a.M, step = (long long)gridDim.x * workers * ROWS;
+  long long r0 = ((long long)blockIdx.x * workers + threadIdx.x / lanes) * ROWS;
+  long long id[ROWS];
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    src[i] = -1;
-    if (r0 + i < n) {
-      const long long id = id_at(a, r0 + i);
-      if (id >= 0 && id < a.vocab) src[i] = (r0 + i) / a.tokens * a.table_stride + id * a.d;
-    }
-  }
-  for (int col = lane * VW; col < a.d; col += lanes * VW) {
-    float v[ROWS][VW];
+  for (int i = 0; i < ROWS; ++i) id[i] = r0 + i < n ? id_at(a, r0 + i) : -1;
+  for (; r0 < n; r0 += step) {
+    long long src[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-#pragma unroll
-      for (int j = 0; j < VW; ++j) v[i][j] = 0.f;
-      if (src[i] >= 0) load_wide<TT, VW>(static_cast<const TT *>(a.table) + src[i] + col, v[i]);
+      src[i] = id[i] >= 0 && id[i] < a.vocab ? (a.M == 1 ? 0 : (r0 + i) / a.tokens * a.table_stride) + id[i] * a.d : -1;
+      id[i] = r0 + step + i < n ? id_at(a, r0 + step + i) : -1;
     }
+    for (int col = lane * VW; col < a.d; col += lanes * VW) {
+      float v[ROWS][VW];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i)
-      if (r0 + i < n) {
+      for (int i = 0; i < ROWS; ++i) {
 #pragma unroll
-        for (int j = 0; j < VW; ++j) v[i][j] *= a.scale;
-        store_wide<AT, VW>(static_cast<AT *>(a.out) + (r0 + i) * a.row_stride + col, v[i]);
+        for (int j = 0; j < VW; ++j) v[i][j] = 0.f;
+        if (src[i] >= 0) load_wide<TT, VW>(static_cast<const TT *>(a.table) + src[i] + col, v[i]);
       }
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i)
+        if (r0 + i < n) {
+#pragma unroll
+          for (int j = 0; j < VW; ++j) v[i][j] *= a.scale;
+          store_wide<AT, VW>(static_cast<AT *>(a.out) + (r0 + i) * a.row_stride + col, v[i]);
+        }
+    }
   }
 }
 
@@ -263,6 +270,19 @@ __global__ void __launch_bounds__(256) embed_buckets_kernel(const EmbedArgs a) {
       __syncwarp();
     }
   }
+  if (a.accumulate) return;
+  const long long row_bytes = (long long)a.d * a.grad_bytes;
+  char *table = static_cast<char *>(a.dtable) + m * a.grad_stride * a.grad_bytes;
+  const bool wide = row_bytes % 16 == 0 && reinterpret_cast<uintptr_t>(table) % 16 == 0;
+  for (int i = warp; i < ids; i += 8) {
+    const long long v = b + (long long)i * kBuckets;
+    if (a.count[m * a.vocab + v] != 0) continue; // this block's own stores, before its last barrier
+    char *row = table + v * row_bytes;
+    if (wide)
+      for (long long o = lane * 16; o < row_bytes; o += 512) *reinterpret_cast<uint4 *>(row + o) = make_uint4(0, 0, 0, 0);
+    else
+      for (long long o = lane * 2; o < row_bytes; o += 64) *reinterpret_cast<unsigned short *>(row + o) = 0;
+  }
 }
 
 // ------------------------------------------------------------------------------------- sums
@@ -279,23 +299,12 @@ template <typename GT, int VW> __device__ __forceinline__ void put_row(const Emb
   store_wide<GT, VW>(p, acc);
 }
 
-// Blocks [0, sum_blocks): chunks, `lanes` threads each and VW columns a thread (blockIdx.z: further columns).
-// The other blocks zero the rows of ids that no token has.
+// Chunks, `lanes` threads each and VW columns a thread (blockIdx.z: further columns).
 template <typename AT, typename GT, int VW>
-__global__ void __launch_bounds__(kWorkThreads) embed_sums_kernel(const EmbedArgs a, int lanes, int sum_blocks) {
+__global__ void __launch_bounds__(kWorkThreads) embed_sums_kernel(const EmbedArgs a, int lanes) {
   const int m = blockIdx.y, lane = threadIdx.x % lanes, worker = threadIdx.x / lanes, workers = kWorkThreads / lanes;
   const int col = (blockIdx.z * lanes + lane) * VW;
   grid_wait();
-  if ((int)blockIdx.x >= sum_blocks) {
-    if (col >= a.d) return;
-    float zero[VW];
-#pragma unroll
-    for (int j = 0; j < VW; ++j) zero[j] = 0.f;
-    for (long long v = (long long)(blockIdx.x - sum_blocks) * workers + worker; v < a.vocab; v += (long long)(gridDim.x - sum_blocks) * workers)
-      if (a.count[m * a.vocab + v] == 0)
-        store_wide<GT, VW>(static_cast<GT *>(a.dtable) + m * a.grad_stride + v * a.d + col, zero);
-    return;
-  }
   const unsigned total = a.total[m];
   const uint2 *sorted = a.sorted + m * a.tokens;
   const AT *dout = static_cast<const AT *>(a.dout) + m * a.tokens * a.row_stride + col;
@@ -358,7 +367,7 @@ __global__ void __launch_bounds__(kWorkThreads) embed_join_kernel(const EmbedArg
   float acc[VW];
   load_wide<float, VW>(part + (chunk * 2 + 1) * a.d, acc);
   const long long to = last / a.C;
-#pragma unroll 4
+#pragma unroll 8
   for (long long c = chunk + 1; c <= to; ++c) {
     float v[VW];
     load_wide<float, VW>(part + c * 2 * a.d, v);
@@ -457,12 +466,13 @@ int diloco_embedding_forward(const diloco_embedding_t *e, const void *ids, const
   EmbedArgs a = args_of(e);
   a.ids = ids, a.table = table, a.out = out;
   const bool wide = e->d % 8 == 0 && e->table_stride % 8 == 0 && e->row_stride % 8 == 0 && aligned_to(table, 16) && aligned_to(out, 16);
+  const int sms = sm_count(pc.device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   with_types(e->table_dtype, e->act_dtype, wide, [&](auto t, auto o, auto w) {
-    constexpr int ROWS = 2;
+    constexpr int ROWS = 4;
     const int lanes = lanes_for(e->d, w.value);
-    const int64_t workers = kWorkThreads / lanes, n = e->tokens * e->M;
-    const int64_t grid = (n + workers * ROWS - 1) / (workers * ROWS);
+    const int64_t workers = kWorkThreads / lanes, n = e->tokens * e->M, most = (int64_t)sms * 8;
+    const int64_t want = (n + workers * ROWS - 1) / (workers * ROWS), grid = want < most ? want : most;
     embed_forward_kernel<decltype(t), decltype(o), w.value, ROWS><<<(unsigned)grid, kWorkThreads, 0, st>>>(a, lanes);
   });
   return launched();
@@ -488,6 +498,7 @@ int diloco_embedding_backward(const diloco_embedding_t *e, const void *ids, cons
   char *ws = static_cast<char *>(workspace);
   EmbedArgs a = args_of(e);
   a.ids = ids, a.dout = dout, a.dtable = dtable, a.accumulate = accumulate != 0;
+  a.grad_bytes = (int)dtype_bytes(e->grad_dtype);
   a.tile_sorted = reinterpret_cast<uint2 *>(ws + l.tile_sorted), a.gathered = reinterpret_cast<uint2 *>(ws + l.gathered);
   a.sorted = reinterpret_cast<uint2 *>(ws + l.sorted), a.tile_off = reinterpret_cast<unsigned *>(ws + l.tile_off);
   a.count = reinterpret_cast<unsigned *>(ws + l.count), a.start = reinterpret_cast<unsigned *>(ws + l.start);
@@ -503,16 +514,12 @@ int diloco_embedding_backward(const diloco_embedding_t *e, const void *ids, cons
   if (rc != DILOCO_OK) return rc;
   const bool wide = e->d % 8 == 0 && e->grad_stride % 8 == 0 && e->row_stride % 8 == 0 && aligned_to(dtable, 16) &&
                     (e->tokens == 0 || aligned_to(dout, 16));
-  const int sms = sm_count(pc.device);
   with_types(e->act_dtype, e->grad_dtype, wide, [&](auto t, auto g, auto w) {
     const int lanes = lanes_for(e->d, w.value), workers = kWorkThreads / lanes;
     const int slabs = (e->d + lanes * w.value - 1) / (lanes * w.value);
     const int sums = (l.chunks + workers - 1) / workers;
-    const int64_t rows = (e->vocab + workers - 1) / workers, most = (int64_t)sms * 4;
-    const int zeros = a.accumulate ? 0 : (int)(rows < most ? rows : most);
-    if (sums + zeros == 0) return;
-    rc = launch_chained(embed_sums_kernel<decltype(t), decltype(g), w.value>, dim3(sums + zeros, e->M, slabs), dim3(kWorkThreads), 0, st, a,
-                        lanes, sums);
+    if (sums == 0) return;
+    rc = launch_chained(embed_sums_kernel<decltype(t), decltype(g), w.value>, dim3(sums, e->M, slabs), dim3(kWorkThreads), 0, st, a, lanes);
     if (rc != DILOCO_OK || l.chunks < 2) return;
     rc = launch_chained(embed_join_kernel<decltype(g), w.value>, dim3(sums, e->M, slabs), dim3(kWorkThreads), 0, st, a, lanes);
   });

@@ -392,14 +392,42 @@ Shape shape_for(int d, int width, bool wide) {
   return {0, SHAPE_LOOP, 0};
 }
 
-template <typename T, typename F> bool with_shape(const Shape &s, F f) {
-  constexpr int W = 16 / (int)sizeof(T);
-  if (s.tpr == SHAPE_LOOP) return false;
-#define DILOCO_NORM_SHAPE(VW_, TPR_, CH_)                                \
-  if (s.vw == VW_ && s.tpr == TPR_ && s.ch == CH_) {                     \
-    f(norm_forward_kernel<T, VW_, TPR_, CH_>, norm_backward_kernel<T, VW_, TPR_, CH_>); \
-    return true;                                                         \
+// Blocks of a kernel that an SM holds at once, asked once.  Grids are that many: what goes beyond runs as a second,
+// thinner wave.
+template <typename K> int ask_resident(K kernel, int threads) {
+  int n = 0;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) != cudaSuccess) {
+    cudaGetLastError();
+    n = 0;
   }
+  return n > 0 ? n : 1;
+}
+
+template <typename T, int VW, int TPR, int CH> struct Kernels {
+  static constexpr int kThreads = Block<TPR>::kThreads, kVectors = kThreads / TPR; // vectors of a block at a time
+  static int forward_resident() {
+    static const int n = ask_resident(norm_forward_kernel<T, VW, TPR, CH>, kThreads);
+    return n;
+  }
+  static int backward_resident() {
+    static const int n = ask_resident(norm_backward_kernel<T, VW, TPR, CH>, kThreads);
+    return n;
+  }
+  static void forward(dim3 grid, cudaStream_t s, const NormArgs &a) { norm_forward_kernel<T, VW, TPR, CH><<<grid, kThreads, 0, s>>>(a); }
+  static void backward(dim3 grid, cudaStream_t s, const NormArgs &a) { norm_backward_kernel<T, VW, TPR, CH><<<grid, kThreads, 0, s>>>(a); }
+};
+template <typename T> struct LoopKernels {
+  static constexpr int kThreads = kLoopThreads, kVectors = 1;
+  static int forward_resident() { return 4; }
+  static int backward_resident() { return 2; }
+  static void forward(dim3 grid, cudaStream_t s, const NormArgs &a) { norm_forward_loop_kernel<T><<<grid, kThreads, 0, s>>>(a); }
+  static void backward(dim3 grid, cudaStream_t s, const NormArgs &a) { norm_backward_loop_kernel<T><<<grid, kThreads, 0, s>>>(a); }
+};
+
+template <typename T, typename F> auto with_shape_of(const Shape &s, F f) {
+  constexpr int W = 16 / (int)sizeof(T);
+#define DILOCO_NORM_SHAPE(VW_, TPR_, CH_) \
+  if (s.vw == VW_ && s.tpr == TPR_ && s.ch == CH_) return f(Kernels<T, VW_, TPR_, CH_>{});
   DILOCO_NORM_SHAPE(W, 8, 1)
   DILOCO_NORM_SHAPE(W, 16, 1)
   DILOCO_NORM_SHAPE(W, 32, 1)
@@ -411,7 +439,12 @@ template <typename T, typename F> bool with_shape(const Shape &s, F f) {
   DILOCO_NORM_SHAPE(1, 256, 4)
   DILOCO_NORM_SHAPE(1, 256, 16)
 #undef DILOCO_NORM_SHAPE
-  return false;
+  return f(LoopKernels<T>{});
+}
+template <typename F> auto with_shape(const diloco_layernorm_t *n, bool wide, F f) {
+  const bool f32 = n->act_dtype == DILOCO_DTYPE_F32;
+  const Shape s = shape_for(n->d, f32 ? 4 : 8, wide);
+  return f32 ? with_shape_of<float>(s, f) : with_shape_of<__nv_bfloat16>(s, f);
 }
 
 int valid(const diloco_layernorm_t *n, bool backward) {
@@ -435,13 +468,10 @@ int blocks_for(int R, int M, int per_block, int per_sm, int sms, int least) {
   return (int)(want < 1 ? 1 : want < most ? want : most);
 }
 
-// The backward's blocks are what sizes its workspace, so they follow from the descriptor and the SM count alone.
+// The backward's blocks are what sizes its workspace: they follow from the descriptor and the device alone.
 int backward_blocks(const diloco_layernorm_t *n, int sms, bool wide) {
-  const Shape s = shape_for(n->d, n->act_dtype == DILOCO_DTYPE_F32 ? 4 : 8, wide);
   const int R = (int)(n->rows * n->groups);
-  if (s.tpr == SHAPE_LOOP) return blocks_for(R, n->M, 1, 2, sms, 1);
-  const int nt = s.tpr <= 32 ? 256 : s.tpr;
-  return blocks_for(R, n->M, nt / s.tpr, 1024 / nt < 1 ? 1 : 1024 / nt, sms, 4);
+  return with_shape(n, wide, [&](auto k) { return blocks_for(R, n->M, k.kVectors, k.backward_resident(), sms, 4); });
 }
 
 int current_sms(int *sms) {
@@ -479,19 +509,10 @@ int diloco_layernorm_forward(const diloco_layernorm_t *n, const void *x, const v
   const int width = (int)(16 / ea);
   const bool wide = aligned_to(x, 16) && aligned_to(y, 16) && n->d % width == 0 && multiple(a.x_row, a.x_group, width) &&
                     multiple(a.y_row, a.y_group, width);
-  const Shape s = shape_for(n->d, width, wide);
   const int sms = sm_count(pc.device);
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  auto go = [&](auto f, auto) {
-    const int nt = s.tpr <= 32 ? 256 : s.tpr;
-    const int g = blocks_for(R, n->M, nt / s.tpr, 2048 / nt, sms, 1);
-    f<<<dim3(g, n->M), nt, 0, st>>>(a);
-  };
-  if (n->act_dtype == DILOCO_DTYPE_F32) {
-    if (!with_shape<float>(s, go)) norm_forward_loop_kernel<float><<<dim3(blocks_for(R, n->M, 1, 4, sms, 1), n->M), kLoopThreads, 0, st>>>(a);
-  } else {
-    if (!with_shape<__nv_bfloat16>(s, go)) norm_forward_loop_kernel<__nv_bfloat16><<<dim3(blocks_for(R, n->M, 1, 4, sms, 1), n->M), kLoopThreads, 0, st>>>(a);
-  }
+  with_shape(n, wide, [&](auto k) {
+    k.forward(dim3(blocks_for(R, n->M, k.kVectors, k.forward_resident(), sms, 1), n->M), static_cast<cudaStream_t>(stream), a);
+  });
   return launched();
 }
 
@@ -526,18 +547,12 @@ int diloco_layernorm_backward(const diloco_layernorm_t *n, const void *dy, const
   a.param_bf16 = n->param_dtype == DILOCO_DTYPE_BF16, a.want_params = want, a.part = static_cast<float *>(workspace);
   const bool wide = aligned_to(x, 16) && aligned_to(dy, 16) && aligned_to(dx, 16) && n->d % width == 0 &&
                     multiple(a.x_row, a.x_group, width) && multiple(a.y_row, a.y_group, width) && multiple(a.dx_row, a.dx_group, width);
-  const Shape s = shape_for(n->d, width, wide);
   const int g = backward_blocks(n, sms, wide);
   if (want && workspace_bytes < (int64_t)g * n->M * 2 * n->d * (int64_t)sizeof(float)) return DILOCO_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int parts = 0;
   if (R) {
-    auto go = [&](auto, auto f) { f<<<dim3(g, n->M), s.tpr <= 32 ? 256 : s.tpr, 0, st>>>(a); };
-    if (n->act_dtype == DILOCO_DTYPE_F32) {
-      if (!with_shape<float>(s, go)) norm_backward_loop_kernel<float><<<dim3(g, n->M), kLoopThreads, 0, st>>>(a);
-    } else {
-      if (!with_shape<__nv_bfloat16>(s, go)) norm_backward_loop_kernel<__nv_bfloat16><<<dim3(g, n->M), kLoopThreads, 0, st>>>(a);
-    }
+    with_shape(n, wide, [&](auto k) { k.backward(dim3(g, n->M), st, a); });
     rc = launched();
     if (rc != DILOCO_OK) return rc;
     parts = g;
