@@ -32,15 +32,16 @@ struct DistillArgs {
   float temperature, inv_t, z, grad_scale;
 };
 
-// The teacher's side of one row in shared memory, k entries each.
+// The teacher's side of one row in shared memory, k entries each, rounded up to whole 16-byte units.
 constexpr int kMaxK = 1024;
+__host__ __device__ constexpr int teacher_entries(int k) { return (k + 3) / 4 * 4; }
+__host__ __device__ constexpr int teacher_bytes(int k) { return 12 * teacher_entries(k); }
 struct Teacher {
   int *id;      // -1: unused
   float *p, *x; // t / T, then the share of the entry; the student's logit there
   __device__ __forceinline__ Teacher(unsigned char *at, int k)
-      : id(reinterpret_cast<int *>(at)), p(reinterpret_cast<float *>(at) + k), x(reinterpret_cast<float *>(at) + 2 * k) {}
+      : id(reinterpret_cast<int *>(at)), p(reinterpret_cast<float *>(at) + teacher_entries(k)), x(p + teacher_entries(k)) {}
 };
-constexpr int teacher_bytes(int k) { return 12 * k; }
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -79,6 +80,7 @@ template <typename T> __device__ __forceinline__ float read_teacher(const Distil
     t.x[i] = x[0];
     if (id >= 0) top = fmaxf(top, q), mine = true;
   }
+  if (lane < teacher_entries(a.k) - a.k) t.id[a.k + lane] = -1;
   any = __any_sync(0xffffffffu, mine);
   top = warp_max(top);
   for (int i = lane; i < a.k; i += 32)
@@ -123,12 +125,20 @@ template <typename T> __device__ __forceinline__ void put_teacher(const DistillA
     const int id = t.id[i];
     if (id < 0) continue;
     bool first = true;
-    float p = 0.f;
-    for (int j = 0; j < a.k; ++j)
-      if (t.id[j] == id) {
-        if (j < i) first = false;
-        p += t.p[j];
+    float p = t.p[i];
+    const int4 *all = reinterpret_cast<const int4 *>(t.id);
+#pragma unroll 4
+    for (int j = 0; j < a.k; j += 4) {
+      const int4 o = all[j / 4];
+      const bool hit[4] = {o.x == id && j != i, o.y == id && j + 1 != i, o.z == id && j + 2 != i, o.w == id && j + 3 != i};
+      if (hit[0] || hit[1] || hit[2] || hit[3]) {
+        for (int e = 0; e < 4; ++e)
+          if (hit[e]) {
+            if (j + e < i) first = false;
+            p += t.p[j + e];
+          }
       }
+    }
     if (!first) continue;
     const float g[1] = {term(t.x[i], a.inv_t * kLog2e, r) - r.wt * p};
     store_vec<T, 1>(grad + id, g);
@@ -151,6 +161,7 @@ template <typename T, int W> __device__ __forceinline__ Span span_of(const T *ro
 
 // Barriers of a block whose warps come to them at different places of the program: plain ones by number.  (A reducing
 // barrier such as __syncthreads_or has to be one and the same instruction for the whole block.)
+template <int ID, int NT> __device__ __forceinline__ void block_arrive() { asm volatile("barrier.cta.arrive %0, %1;" ::"n"(ID), "n"(NT) : "memory"); }
 template <int ID, int NT> __device__ __forceinline__ void block_sync() { asm volatile("barrier.cta.sync %0, %1;" ::"n"(ID), "n"(NT) : "memory"); }
 
 // What the warps of a row leave for each other before the first barrier.
@@ -220,31 +231,39 @@ __device__ __forceinline__ uint4 terms(const uint4 &r, float2 c, float2 lse2, fl
 
 // Rows of at most (NT - 32) * RV accesses: NT - 32 threads for the row, the last warp for the teacher.  The next row is
 // on its way into shared memory (each thread copies what it will itself read, so no barrier is needed) while this
-// one is worked on.  Two barriers a row: sums and teacher are known; the row's gradient is written.
+// one is worked on.  The row's threads wait at one barrier a row, for the sums of all warps; the teacher's warp
+// reads the next row's entries behind it, waits for the row's gradient and writes its elements.
 template <typename T, int NT, int RV>
 __global__ void __launch_bounds__(NT, 512 / NT) distill_resident_kernel(const DistillArgs a) {
   constexpr int W = 16 / (int)sizeof(T), NC = NT - 32;
   using Raw = typename Pack<T, W>::raw;
-  extern __shared__ __align__(16) unsigned char staged[]; // [RV][NC] accesses, then the teacher
-  __shared__ Partial red;
+  extern __shared__ __align__(16) unsigned char staged[]; // [RV][NC] accesses, then two rows' teachers
+  __shared__ Partial red[2]; // rows in turn
   const int tid = threadIdx.x;
   const float c = a.inv_t * kLog2e;
   auto row_of = [&](long long n) { return static_cast<const T *>(a.logits) + n * a.logits_stride; };
   auto weight_of = [&](long long n) { return a.grad_scale * (a.row_weight ? a.row_weight[n] : 1.f); };
+  long long n = blockIdx.x;
+  int turn = 0;
   if (tid >= NC) {
-    const Teacher t(staged + NC * RV * 16, a.k);
-    for (long long n = blockIdx.x; n < a.rows; n += gridDim.x) {
-      bool any;
-      const float kl = read_teacher<T>(a, t, n, row_of(n), any);
+    unsigned char *const at = staged + NC * RV * 16;
+    bool any = false;
+    float kl = 0.f;
+    if (n < a.rows) kl = read_teacher<T>(a, Teacher(at, a.k), n, row_of(n), any);
+    for (; n < a.rows; n += gridDim.x, turn ^= 1) {
+      const Teacher t(at + turn * teacher_bytes(a.k), a.k);
       const float wn = weight_of(n);
-      if (tid == NC) red.any = any;
+      if (tid == NC) red[turn].any = any;
       block_sync<1, NT>();
       float m, s;
-      get_partial(red, NC / 32, m, s);
+      get_partial(red[turn], NC / 32, m, s);
       const RowScale r = row_scale(a, m, s, wn, any);
       put_loss(a, n, r, kl, wn, any);
+      const bool put = a.dlogits && any;
+      if (n + gridDim.x < a.rows)
+        kl = read_teacher<T>(a, Teacher(at + (turn ^ 1) * teacher_bytes(a.k), a.k), n + gridDim.x, row_of(n + gridDim.x), any);
       block_sync<2, NT>();
-      if (a.dlogits && any) put_teacher<T>(a, t, static_cast<T *>(a.dlogits) + n * a.grad_stride, r);
+      if (put) put_teacher<T>(a, t, static_cast<T *>(a.dlogits) + n * a.grad_stride, r);
       __syncwarp();
     }
     return;
@@ -259,14 +278,13 @@ __global__ void __launch_bounds__(NT, 512 / NT) distill_resident_kernel(const Di
       if (i * NC + tid < sp.body) copy_async16(to + i * NC * 16, row + sp.head + (long long)(i * NC + tid) * W);
     copy_commit();
   };
-  long long n = blockIdx.x;
   if (n >= a.rows) return;
   Span sp = span_of<T, W>(row_of(n), a.vocab);
   fetch(row_of(n), sp);
   int odd = odd_of(sp);
   float single[1] = {-INFINITY};
   if (odd >= 0) load_vec<T, 1>(row_of(n) + odd, single);
-  while (n < a.rows) {
+  for (; n < a.rows; turn ^= 1) {
     const long long next = n + gridDim.x;
     const float wn = weight_of(n), one = single[0];
     const int at = odd;
@@ -295,12 +313,12 @@ __global__ void __launch_bounds__(NT, 512 / NT) distill_resident_kernel(const Di
 #pragma unroll
     for (int i = 0; i < RV; ++i)
       if (i * NC + tid < body) add_terms(raw[i], cc, mm, two);
-    put_partial(red, m, two.x + two.y);
+    put_partial(red[turn], m, two.x + two.y);
     block_sync<1, NT>();
     if (a.dlogits) {
       float s;
-      get_partial(red, NC / 32, m, s);
-      const bool any = red.any != 0;
+      get_partial(red[turn], NC / 32, m, s);
+      const bool any = red[turn].any != 0;
       const RowScale r = row_scale(a, m, s, wn, any);
       T *grad = static_cast<T *>(a.dlogits) + n * a.grad_stride;
       const float2 lse2 = make_float2(-r.lse2, -r.lse2), coef = make_float2(r.coef, r.coef);
@@ -313,7 +331,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) distill_resident_kernel(const Di
         store_vec<T, 1>(grad + at, x);
       }
     }
-    block_sync<2, NT>(); // the row is written, `red` is read
+    block_arrive<2, NT>(); // the row is written
     n = next;
   }
 }
@@ -398,9 +416,9 @@ int valid(const diloco_distill_t *l) {
 constexpr int kHeld = 18; // accesses a thread holds: 72 registers of 128
 template <typename T, int NT> int launch_resident(const DistillArgs &a, int sms, cudaStream_t s) {
   constexpr int kRow = (NT - 32) * kHeld * 16;
-  const int bytes = kRow + teacher_bytes(a.k);
+  const int bytes = kRow + 2 * teacher_bytes(a.k);
   static const bool ok = cudaFuncSetAttribute(distill_resident_kernel<T, NT, kHeld>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                              kRow + teacher_bytes(kMaxK)) == cudaSuccess;
+                                              kRow + 2 * teacher_bytes(kMaxK)) == cudaSuccess;
   if (!ok) return cuda_fail(cudaGetLastError());
   // 128 registers a thread and this shared memory: blocks that an SM holds
   const int by_smem = (227 * 1024) / (bytes + 2048), per_sm = by_smem < 512 / NT ? by_smem : 512 / NT;
