@@ -512,7 +512,7 @@ enum { DILOCO_DTYPE_F32 = 0, DILOCO_DTYPE_BF16 = 1 };
  * backward sorts each replica's tokens by id (stable) and sums each row's terms in fp32 in an order that
  * depends on the ids alone.  accumulate = 0 writes every row of dtable (zero for ids that do not
  * appear), accumulate != 0 touches only rows that appear: the form for a table that is also the output
- * projection, whose dense gradient is already there.  vocab <= 2^20, M * tokens < 2^31.
+ * projection, whose dense gradient is already there.  vocab <= 2^20, M * tokens <= 2^30.
  * The workspace's size is diloco_embedding_workspace_bytes (negative: a status).
  */
 typedef struct {
@@ -542,7 +542,8 @@ int diloco_embedding_backward(const diloco_embedding_t *e, const void *ids, cons
  * mean and rstd are fp32, [M, rows, groups] contiguous; forward writes them where they are not NULL, backward
  * reads them.  Vector (r, g) of replica m starts at (m rows + r) row_stride + g group_stride of its tensor, so q
  * and k are normalised in place inside a fused projection's rows.  bias and dbias may be NULL; backward may be
- * called without dweight and dbias.  y may be x and dx may be dy (same strides).  d <= 65536.
+ * called without dweight and dbias.  y may be x and dx may be dy (same strides).  d <= 65536,
+ * rows * groups <= 2^30.
  */
 typedef struct {
   int32_t M, d, groups;

@@ -499,13 +499,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 }
 
 template <int HD> int launch(const AttnArgs &a, const HeadMap &mq, const HeadMap &mk, const HeadMap &mv, const HeadMap &mdo, cudaStream_t s) {
-  const int bytes = BwdLayout<HD>::kBytes;
-  cudaError_t e = cudaFuncSetAttribute(attn_dq_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_dkv_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    return cuda_fail(e);
-  }
+  constexpr int bytes = BwdLayout<HD>::kBytes;
+  static OncePerDevice once;
+  if (!once.get([] { return allow_smem(attn_dq_kernel<HD>, bytes) && allow_smem(attn_dkv_kernel<HD>, bytes); })) return DILOCO_ERR_CUDA;
   const long long slots = (long long)a.tokens / kRows + a.sequences + 1;
   if (slots * a.heads > INT32_MAX) return DILOCO_ERR_UNSUPPORTED;
   attn_dq_kernel<HD><<<(unsigned)(slots * a.heads), kBwdThreads, bytes, s>>>(a, mq, mk, mv, mdo, (int)slots);

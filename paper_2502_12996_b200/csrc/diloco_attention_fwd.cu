@@ -278,11 +278,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
 
 template <int HD> int launch(const AttnArgs &a, const HeadMap &mq, const HeadMap &mk, const HeadMap &mv, cudaStream_t s) {
   auto kernel = attn_forward_kernel<HD>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdLayout<HD>::kBytes);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    return cuda_fail(e);
-  }
+  static OncePerDevice once;
+  if (!once.get([&] { return allow_smem(kernel, FwdLayout<HD>::kBytes); })) return DILOCO_ERR_CUDA;
   const long long slots = (long long)a.tokens / (2 * kRows) + a.sequences + 1;
   if (slots * a.heads > INT32_MAX) return DILOCO_ERR_UNSUPPORTED;
   kernel<<<(unsigned)(slots * a.heads), kFwdThreads, FwdLayout<HD>::kBytes, s>>>(a, mq, mk, mv, (int)slots, a.scale < 0.f);

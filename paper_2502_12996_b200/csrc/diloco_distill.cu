@@ -183,12 +183,6 @@ __device__ __forceinline__ void get_partial(const Partial &red, int warps, float
   s = warp_sum(bm == -INFINITY ? bs : bs * ex2(bm - m)); // bm = -inf: bs is 0, or NaN
 }
 
-__device__ __forceinline__ void copy_async16(unsigned smem, const void *g) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(g) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
-
 // The largest of an access's elements
 __device__ __forceinline__ float pack_max(const float4 &r) { return fmaxf(fmaxf(r.x, r.y), fmaxf(r.z, r.w)); }
 __device__ __forceinline__ float pack_max(const uint4 &r) {
@@ -417,9 +411,8 @@ constexpr int kHeld = 18; // accesses a thread holds: 72 registers of 128
 template <typename T, int NT> int launch_resident(const DistillArgs &a, int sms, cudaStream_t s) {
   constexpr int kRow = (NT - 32) * kHeld * 16;
   const int bytes = kRow + 2 * teacher_bytes(a.k);
-  static const bool ok = cudaFuncSetAttribute(distill_resident_kernel<T, NT, kHeld>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                              kRow + 2 * teacher_bytes(kMaxK)) == cudaSuccess;
-  if (!ok) return cuda_fail(cudaGetLastError());
+  static OncePerDevice once;
+  if (!once.get([] { return allow_smem(distill_resident_kernel<T, NT, kHeld>, kRow + 2 * teacher_bytes(kMaxK)); })) return DILOCO_ERR_CUDA;
   // 128 registers a thread and this shared memory: blocks that an SM holds
   const int by_smem = (227 * 1024) / (bytes + 2048), per_sm = by_smem < 512 / NT ? by_smem : 512 / NT;
   const long long most = (long long)sms * (per_sm < 1 ? 1 : per_sm);

@@ -49,23 +49,26 @@ __device__ __forceinline__ long long id_at(const EmbedArgs &a, long long i) {
 }
 
 // ---------------------------------------------------------------------------------- forward
-// A worker (`lanes` threads) takes ROWS tokens at a time, so that as many rows are in flight at once, and reads the
-// next ones' ids before it waits for these rows.  Blocks stay (8 on an SM): with a block for every 2 rows each, the
-// wait for the ids was not hidden and 65536 rows of 4 KB took 100 us.
+// A worker (`lanes` threads) takes ROWS tokens of one replica (blockIdx.y) at a time, so that as many rows are in
+// flight at once, and reads the next ones' ids before it waits for these rows.  Blocks stay (8 on an SM): with a
+// block for every 2 rows the wait for the ids was not hidden and 65536 rows of 4 KB took 100 us.
 template <typename TT, typename AT, int VW, int ROWS>
 __global__ void __launch_bounds__(kWorkThreads) embed_forward_kernel(const EmbedArgs a, int lanes) {
-  const int lane = threadIdx.x % lanes, workers = kWorkThreads / lanes;
-  const long long n = a.tokens * a.M, step = (long long)gridDim.x * workers * ROWS;
-  long long r0 = ((long long)blockIdx.x * workers + threadIdx.x / lanes) * ROWS;
+  const int m = blockIdx.y, lane = threadIdx.x % lanes, workers = kWorkThreads / lanes;
+  const long long first = m * a.tokens;
+  const TT *table = static_cast<const TT *>(a.table) + m * a.table_stride;
+  AT *out = static_cast<AT *>(a.out) + first * a.row_stride;
+  const int n = (int)a.tokens, step = gridDim.x * workers * ROWS;
+  int r0 = (blockIdx.x * workers + threadIdx.x / lanes) * ROWS;
   long long id[ROWS];
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) id[i] = r0 + i < n ? id_at(a, r0 + i) : -1;
+  for (int i = 0; i < ROWS; ++i) id[i] = r0 + i < n ? id_at(a, first + r0 + i) : -1;
   for (; r0 < n; r0 += step) {
     long long src[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-      src[i] = id[i] >= 0 && id[i] < a.vocab ? (a.M == 1 ? 0 : (r0 + i) / a.tokens * a.table_stride) + id[i] * a.d : -1;
-      id[i] = r0 + step + i < n ? id_at(a, r0 + step + i) : -1;
+      src[i] = id[i] >= 0 && id[i] < a.vocab ? id[i] * a.d : -1;
+      id[i] = r0 + step + i < n ? id_at(a, first + r0 + step + i) : -1;
     }
     for (int col = lane * VW; col < a.d; col += lanes * VW) {
       float v[ROWS][VW];
@@ -73,14 +76,13 @@ __global__ void __launch_bounds__(kWorkThreads) embed_forward_kernel(const Embed
       for (int i = 0; i < ROWS; ++i) {
 #pragma unroll
         for (int j = 0; j < VW; ++j) v[i][j] = 0.f;
-        if (src[i] >= 0) load_wide<TT, VW>(static_cast<const TT *>(a.table) + src[i] + col, v[i]);
+        if (src[i] >= 0) load_wide<TT, VW>(table + src[i] + col, v[i]);
       }
 #pragma unroll
       for (int i = 0; i < ROWS; ++i)
         if (r0 + i < n) {
-#pragma unroll
-          for (int j = 0; j < VW; ++j) v[i][j] *= a.scale;
-          store_wide<AT, VW>(static_cast<AT *>(a.out) + (r0 + i) * a.row_stride + col, v[i]);
+          Each<VW>::mul(v[i], v[i], a.scale);
+          store_wide<AT, VW>(out + (long long)(r0 + i) * a.row_stride + col, v[i]);
         }
     }
   }
@@ -301,7 +303,9 @@ template <typename GT, int VW> __device__ __forceinline__ void put_row(const Emb
 
 // Chunks, `lanes` threads each and VW columns a thread (blockIdx.z: further columns).
 template <typename AT, typename GT, int VW>
-__global__ void __launch_bounds__(kWorkThreads) embed_sums_kernel(const EmbedArgs a, int lanes) {
+__global__ void __launch_bounds__(kWorkThreads, 2) embed_sums_kernel(const EmbedArgs a, int lanes) {
+  constexpr int W = VW * (int)sizeof(AT) <= 16 ? VW : 16 / (int)sizeof(AT); // elements of one access
+  constexpr int ROWS = W == VW ? 8 : 4;                                      // tokens in flight
   const int m = blockIdx.y, lane = threadIdx.x % lanes, worker = threadIdx.x / lanes, workers = kWorkThreads / lanes;
   const int col = (blockIdx.z * lanes + lane) * VW;
   grid_wait();
@@ -310,43 +314,62 @@ __global__ void __launch_bounds__(kWorkThreads) embed_sums_kernel(const EmbedArg
   const AT *dout = static_cast<const AT *>(a.dout) + m * a.tokens * a.row_stride + col;
   const long long chunk = (long long)blockIdx.x * workers + worker;
   const unsigned c0 = chunk < a.chunks ? (unsigned)(chunk * a.C) : total;
-  if (c0 >= total || col >= a.d) return; // whole workers leave, or lanes beyond the row: no warp-wide step follows
+  if (c0 >= total) return; // whole warps: a worker is one warp or several
   const unsigned c1 = min(c0 + a.C, total);
-  bool began = c0 > 0 && sorted[c0 - 1].x == sorted[c0].x;
+  const bool in = col < a.d;
   float acc[VW];
 #pragma unroll
   for (int j = 0; j < VW; ++j) acc[j] = 0.f;
   float *part = a.part + ((long long)m * a.chunks + chunk) * 2 * a.d + col;
-  unsigned cur = sorted[c0].x;
-  for (unsigned e0 = c0; e0 < c1; e0 += 8) {
-    uint2 en[8];
-    float v[8][VW];
+  // lane l of a warp holds entry l of the next 32; the neighbours tell whether a run crosses the chunk's ends
+  const int wl = threadIdx.x & 31;
+  uint2 mine = c0 + wl < c1 ? sorted[c0 + wl] : make_uint2(0, 0);
+  const unsigned before = c0 > 0 ? sorted[c0 - 1].x : 0xffffffffu, after = c1 < total ? sorted[c1].x : 0xffffffffu;
+  unsigned cur = __shfl_sync(0xffffffffu, mine.x, 0);
+  bool began = before == cur;
+  for (unsigned e0 = c0; e0 < c1; e0 += 32) {
+    const uint2 held = mine;
+    if (e0 + 32 + wl < c1) mine = sorted[e0 + 32 + wl];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) en[k] = e0 + k < c1 ? sorted[e0 + k] : make_uint2(cur, 0xffffffffu);
+    for (int b = 0; b < 32; b += ROWS) {
+      if (e0 + b >= c1) break; // the same for the whole warp
+      typename Pack<AT, W>::raw raw[ROWS][VW / W];
+      unsigned id[ROWS];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < ROWS; ++k) {
+        id[k] = __shfl_sync(0xffffffffu, held.x, b + k);
+        const unsigned token = __shfl_sync(0xffffffffu, held.y, b + k);
+        if (in && e0 + b + k < c1)
 #pragma unroll
-      for (int j = 0; j < VW; ++j) v[k][j] = 0.f;
-      if (e0 + k < c1) load_wide<AT, VW>(dout + (long long)en[k].y * a.row_stride, v[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (e0 + k < c1) {
-        if (en[k].x != cur) { // the same for every thread of the worker
-          if (began) store_wide<float, VW>(part, acc);
-          else put_row<GT, VW>(a, m, cur, col, acc);
-          began = false;
-          cur = en[k].x;
-#pragma unroll
-          for (int j = 0; j < VW; ++j) acc[j] = 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < VW; ++j) acc[j] += v[k][j];
+          for (int u = 0; u < VW / W; ++u)
+            raw[k][u] = *reinterpret_cast<const typename Pack<AT, W>::raw *>(dout + (long long)token * a.row_stride + u * W);
       }
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k)
+        if (e0 + b + k < c1) {
+          if (id[k] != cur) { // the same for every thread of the worker
+            if (in) {
+              if (began) store_wide<float, VW>(part, acc);
+              else put_row<GT, VW>(a, m, cur, col, acc);
+            }
+            began = false;
+            cur = id[k];
+#pragma unroll
+            for (int j = 0; j < VW; ++j) acc[j] = 0.f;
+          }
+#pragma unroll
+          for (int u = 0; u < VW / W; ++u) {
+            float v[W];
+            unpack(raw[k][u], v);
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[u * W + j] += v[j];
+          }
+        }
     }
   }
+  if (!in) return;
   if (began) store_wide<float, VW>(part, acc);
-  else if (c1 < total && sorted[c1].x == cur) store_wide<float, VW>(part + a.d, acc);
+  else if (after == cur) store_wide<float, VW>(part + a.d, acc);
   else put_row<GT, VW>(a, m, cur, col, acc);
 }
 
@@ -367,12 +390,15 @@ __global__ void __launch_bounds__(kWorkThreads) embed_join_kernel(const EmbedArg
   float acc[VW];
   load_wide<float, VW>(part + (chunk * 2 + 1) * a.d, acc);
   const long long to = last / a.C;
-#pragma unroll 8
-  for (long long c = chunk + 1; c <= to; ++c) {
-    float v[VW];
-    load_wide<float, VW>(part + c * 2 * a.d, v);
+  constexpr int BATCH = 8; // partial sums in flight: the commonest id of a text has one in every few chunks
+  for (long long c = chunk + 1; c <= to; c += BATCH) {
+    float v[BATCH][VW];
 #pragma unroll
-    for (int j = 0; j < VW; ++j) acc[j] += v[j];
+    for (int k = 0; k < BATCH; ++k)
+      if (c + k <= to) load_wide<float, VW>(part + (c + k) * 2 * a.d, v[k]);
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k)
+      if (c + k <= to) Each<VW>::add(acc, acc, v[k]);
   }
   put_row<GT, VW>(a, m, id, col, acc);
 }
@@ -384,7 +410,7 @@ int valid(const diloco_embedding_t *e) {
   if (e->ids_int64 != 0 && e->ids_int64 != 1) return DILOCO_ERR_INVALID_ARG;
   if (!dtype_ok(e->table_dtype) || !dtype_ok(e->act_dtype) || !dtype_ok(e->grad_dtype)) return DILOCO_ERR_INVALID_ARG;
   if (e->vocab > kMaxVocab || e->M > 65535 || e->d > (1 << 20)) return DILOCO_ERR_UNSUPPORTED;
-  if (e->tokens > INT32_MAX / e->M) return DILOCO_ERR_UNSUPPORTED;
+  if (e->tokens > (1 << 30) / e->M) return DILOCO_ERR_UNSUPPORTED;
   if (e->M > 1 && e->table_stride < e->vocab * e->d) return DILOCO_ERR_INVALID_ARG;
   return DILOCO_OK;
 }
@@ -471,9 +497,9 @@ int diloco_embedding_forward(const diloco_embedding_t *e, const void *ids, const
   with_types(e->table_dtype, e->act_dtype, wide, [&](auto t, auto o, auto w) {
     constexpr int ROWS = 4;
     const int lanes = lanes_for(e->d, w.value);
-    const int64_t workers = kWorkThreads / lanes, n = e->tokens * e->M, most = (int64_t)sms * 8;
-    const int64_t want = (n + workers * ROWS - 1) / (workers * ROWS), grid = want < most ? want : most;
-    embed_forward_kernel<decltype(t), decltype(o), w.value, ROWS><<<(unsigned)grid, kWorkThreads, 0, st>>>(a, lanes);
+    const int64_t workers = kWorkThreads / lanes, want = (e->tokens + workers * ROWS - 1) / (workers * ROWS);
+    const int64_t most = ((int64_t)sms * 8 + e->M - 1) / e->M;
+    embed_forward_kernel<decltype(t), decltype(o), w.value, ROWS><<<dim3((unsigned)(want < most ? want : most), e->M), kWorkThreads, 0, st>>>(a, lanes);
   });
   return launched();
 }

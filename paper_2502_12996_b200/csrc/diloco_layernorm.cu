@@ -7,8 +7,7 @@
 // A pass reads every activation once and writes once (4 bytes of traffic per bf16 element forward, 6
 // backward, against some 10-20 instructions), so memory bounds it and the layout serves the loads: TPR
 // threads hold one vector of d elements in registers, 16 bytes per access and CH accesses per thread, the
-// parameters stay in registers (persistent blocks), and the next vector's loads are issued before this
-// one's sums.  The variance is the two-pass form on the register copy: no cancellation for any mean.
+// parameters stay in registers (persistent blocks), and the next vectors are on their way to shared memory.  The variance is the two-pass form on the register copy: no cancellation for any mean.
 // The weights' gradients are summed in registers over a block's vectors, once per block into the
 // workspace, and joined there in block order by a second small kernel: the same bits every time.
 #include "diloco_ops.cuh"
@@ -24,6 +23,8 @@ struct NormArgs {
   long long x_row, x_group, y_row, y_group, dx_row, dx_group, param_stride;
   int R; // vectors per replica: rows * groups
   int groups, d;
+  unsigned magic; // r / groups = (r * magic) >> 32 >> shift, for r < 2^31
+  int shift;
   float eps;
   int param_bf16, want_params;
 };
@@ -56,20 +57,80 @@ template <int TPR, int N> __device__ __forceinline__ void row_sum(float (&v)[N],
 
 template <int TPR> struct Block { static constexpr int kThreads = TPR <= 32 ? 256 : TPR; };
 
-template <typename T, int VW, int TPR, int CH>
-__global__ void __launch_bounds__(Block<TPR>::kThreads, 1) norm_forward_kernel(const NormArgs a) {
-  constexpr int NT = Block<TPR>::kThreads, RPB = NT / TPR; // vectors of one block at a time
+// The vectors of one thread on their way: a ring of DEPTH rows of N arrays in shared memory, filled by asynchronous
+// 16-byte copies; every thread reads back only what it copied, so there is no barrier, and what is in flight costs no
+// registers (with one row ahead in registers the backward pass had 24 KB in flight on an SM and ran at 3.3 TB/s).
+// Single elements (VW = 1) go through registers, one row ahead.
+template <typename T, int VW, int TPR, int CH, int N> struct Ring {
+  static constexpr int kThreads = Block<TPR>::kThreads;
+  static constexpr bool kStaged = VW * sizeof(T) == 16;
+  static constexpr int kDepth = !kStaged ? 2 : kThreads * CH >= 1024 ? 2 : kThreads * CH >= 512 ? 3 : 4;
+  static constexpr int kBytes = kStaged ? kDepth * N * CH * kThreads * 16 : 0;
   using Raw = typename Pack<T, VW>::raw;
+  Raw ahead[kStaged ? 1 : N][kStaged ? 1 : CH];
+  unsigned char *mine;
+  __device__ __forceinline__ explicit Ring(unsigned char *smem) : mine(smem + threadIdx.x * 16) {}
+  // array n of the row in `slot`; `here`: this thread's first element
+  __device__ __forceinline__ void fetch(int slot, int n, const T *here, const bool (&in)[CH], bool there) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (there && in[c]) {
+        if constexpr (kStaged)
+          copy_async16((unsigned)__cvta_generic_to_shared(mine) + ((slot * N + n) * CH + c) * kThreads * 16, here + c * TPR * VW);
+        else
+          ahead[n][c] = *reinterpret_cast<const Raw *>(here + c * TPR * VW);
+      }
+  }
+  __device__ __forceinline__ void commit() {
+    if constexpr (kStaged) copy_commit();
+  }
+  // rows but the newest kDepth - 1 have landed
+  __device__ __forceinline__ void wait() {
+    if constexpr (kStaged) copy_wait<kDepth - 1>();
+  }
+  // whatever is not there reads as zero
+  __device__ __forceinline__ void read(int slot, int n, int c, float (&v)[VW], bool there) {
+    if (there) {
+      if constexpr (kStaged) unpack(*reinterpret_cast<const Raw *>(mine + ((slot * N + n) * CH + c) * kThreads * 16), v);
+      else unpack(ahead[n][c], v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VW; ++j) v[j] = 0.f;
+    }
+  }
+};
+
+template <typename T, int VW, int TPR, int CH>
+__global__ void __launch_bounds__(Block<TPR>::kThreads, VW * CH > 8 && VW > 1 ? 512 / Block<TPR>::kThreads : 1) norm_forward_kernel(const NormArgs a) {
+  constexpr int NT = Block<TPR>::kThreads, RPB = NT / TPR; // vectors of one block at a time
+  using R = Ring<T, VW, TPR, CH, 1>;
+  using E = Each<VW>;
+  extern __shared__ __align__(16) unsigned char staged[];
   __shared__ float buf[4][TPR > 32 ? TPR / 32 : 1][1];
   const int m = blockIdx.y, lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   const T *x = static_cast<const T *>(a.x);
   T *y = static_cast<T *>(a.y);
   bool in[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) in[c] = (c * TPR + lane) * VW < a.d;
+  const long long first = (long long)m * (a.R / a.groups); // row of the tensor
+  auto where = [&](int r, long long row_stride, long long group_stride) {
+    const int row = a.groups == 1 ? r : (int)(__umulhi((unsigned)r, a.magic) >> a.shift), g = r - row * a.groups;
+    return (first + row) * row_stride + g * group_stride + lane * VW;
+  };
+  R ring(staged);
+  const int step = gridDim.x * RPB;
+  auto fetch = [&](int r, int slot) {
+    ring.fetch(slot, 0, r < a.R ? x + where(r, a.x_row, a.x_group) : x, in, r < a.R);
+    ring.commit();
+  };
+  int r = blockIdx.x * RPB + sub;
+#pragma unroll
+  for (int k = 0; k < R::kDepth - 1; ++k) fetch(r + k * step, k);
   float w[CH][VW], b[CH][VW];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int col = (c * TPR + lane) * VW;
-    in[c] = col < a.d;
 #pragma unroll
     for (int j = 0; j < VW; ++j) {
       w[c][j] = in[c] ? param_at(a.w, a.param_bf16, m * a.param_stride + col + j) : 0.f;
@@ -77,55 +138,42 @@ __global__ void __launch_bounds__(Block<TPR>::kThreads, 1) norm_forward_kernel(c
     }
   }
   const float inv_d = 1.f / (float)a.d;
-  auto where = [&](int r, long long row_stride, long long group_stride) {
-    const int row = r / a.groups, g = r - row * a.groups;
-    const long long mr = (long long)m * (a.R / a.groups) + row;
-    return mr * row_stride + g * group_stride + lane * VW;
-  };
-  Raw next[CH];
-  auto fetch = [&](int r) {
-    if (r < a.R) {
-      const T *p = x + where(r, a.x_row, a.x_group);
+  int half = 0, slot = 0;
+  for (int r0 = blockIdx.x * RPB; r0 < a.R; r0 += step, r += step) { // the same trips for every thread of the block
+    float v[CH][VW], s[1], sq[VW];
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
-        if (in[c]) next[c] = *reinterpret_cast<const Raw *>(p + c * TPR * VW);
+    for (int j = 0; j < VW; ++j) sq[j] = 0.f;
+    if constexpr (R::kStaged) {
+      fetch(r + (R::kDepth - 1) * step, slot == 0 ? R::kDepth - 1 : slot - 1);
+      ring.wait();
     }
-  };
-  const int step = gridDim.x * RPB;
-  int half = 0;
-  fetch(blockIdx.x * RPB + sub);
-  for (int r0 = blockIdx.x * RPB; r0 < a.R; r0 += step) { // the same trips for every thread of the block
-    const int r = r0 + sub;
-    float v[CH][VW], s[1] = {0.f};
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      unpack(next[c], v[c]);
-#pragma unroll
-      for (int j = 0; j < VW; ++j) {
-        if (!in[c] || r >= a.R) v[c][j] = 0.f;
-        s[0] += v[c][j];
-      }
+      ring.read(slot, 0, c, v[c], in[c] && r < a.R);
+      E::add(sq, sq, v[c]);
     }
-    fetch(r + step);
+    s[0] = E::sum(sq);
+    if constexpr (!R::kStaged) fetch(r + step, 0);
+    slot = slot + 1 == R::kDepth ? 0 : slot + 1;
     row_sum<TPR>(s, buf[half]);
     const float mean = s[0] * inv_d;
-    s[0] = 0.f;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int j = 0; j < VW; ++j) sq[j] = 0.f;
 #pragma unroll
-      for (int j = 0; j < VW; ++j) {
-        v[c][j] -= mean;
-        if (in[c]) s[0] = fmaf(v[c][j], v[c][j], s[0]);
-      }
+    for (int c = 0; c < CH; ++c) {
+      E::add(v[c], v[c], -mean);
+      if (in[c]) E::fma(sq, v[c], v[c], sq);
+    }
+    s[0] = E::sum(sq);
     row_sum<TPR>(s, buf[half + 1]);
     half ^= 2;
-    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_d, a.eps));
+    const float rstd = rsqrtf(fmaf(s[0], inv_d, a.eps));
     if (r < a.R) {
       T *p = y + where(r, a.y_row, a.y_group);
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-#pragma unroll
-        for (int j = 0; j < VW; ++j) v[c][j] = fmaf(w[c][j], v[c][j] * rstd, b[c][j]);
+        E::mul(v[c], v[c], rstd);
+        E::fma(v[c], v[c], w[c], b[c]);
         if (in[c]) store_vec<T, VW>(p + c * TPR * VW, v[c]);
       }
       if (lane == 0) {
@@ -138,9 +186,11 @@ __global__ void __launch_bounds__(Block<TPR>::kThreads, 1) norm_forward_kernel(c
 }
 
 template <typename T, int VW, int TPR, int CH>
-__global__ void __launch_bounds__(Block<TPR>::kThreads, 1) norm_backward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(Block<TPR>::kThreads, VW * CH > 8 && VW > 1 ? 512 / Block<TPR>::kThreads : 1) norm_backward_kernel(const NormArgs a) {
   constexpr int NT = Block<TPR>::kThreads, RPB = NT / TPR;
-  using Raw = typename Pack<T, VW>::raw;
+  using R = Ring<T, VW, TPR, CH, 2>;
+  using E = Each<VW>;
+  extern __shared__ __align__(16) unsigned char staged[];
   __shared__ float buf[2][TPR > 32 ? TPR / 32 : 1][2];
   // the vectors of a block that a warp or less holds meet here: [2, d] sums, d <= TPR * VW * CH
   __shared__ float join[RPB > 1 ? 2 * TPR * VW * CH : 1];
@@ -148,11 +198,31 @@ __global__ void __launch_bounds__(Block<TPR>::kThreads, 1) norm_backward_kernel(
   const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
   T *dx = static_cast<T *>(a.dx);
   bool in[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) in[c] = (c * TPR + lane) * VW < a.d;
+  const long long first = (long long)m * (a.R / a.groups); // row of the tensor
+  auto where = [&](int r, long long row_stride, long long group_stride) {
+    const int row = a.groups == 1 ? r : (int)(__umulhi((unsigned)r, a.magic) >> a.shift), g = r - row * a.groups;
+    return (first + row) * row_stride + g * group_stride + lane * VW;
+  };
+  R ring(staged);
+  const int step = gridDim.x * RPB;
+  auto fetch = [&](int r, int slot) {
+    const bool there = r < a.R;
+    ring.fetch(slot, 0, there ? x + where(r, a.x_row, a.x_group) : x, in, there);
+    ring.fetch(slot, 1, there ? dy + where(r, a.y_row, a.y_group) : dy, in, there);
+    ring.commit();
+  };
+  int r = blockIdx.x * RPB + sub;
+#pragma unroll
+  for (int k = 0; k < R::kDepth - 1; ++k) fetch(r + k * step, k);
+  const long long stat = (long long)m * a.R;
+  float nmean = 0.f, nrstd = 0.f;
+  if (r < a.R) nmean = a.mean[stat + r], nrstd = a.rstd[stat + r];
   float w[CH][VW], dw[CH][VW], db[CH][VW];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int col = (c * TPR + lane) * VW;
-    in[c] = col < a.d;
 #pragma unroll
     for (int j = 0; j < VW; ++j) {
       w[c][j] = in[c] ? param_at(a.w, a.param_bf16, m * a.param_stride + col + j) : 0.f;
@@ -160,61 +230,45 @@ __global__ void __launch_bounds__(Block<TPR>::kThreads, 1) norm_backward_kernel(
     }
   }
   const float inv_d = 1.f / (float)a.d;
-  auto where = [&](int r, long long row_stride, long long group_stride) {
-    const int row = r / a.groups, g = r - row * a.groups;
-    const long long mr = (long long)m * (a.R / a.groups) + row;
-    return mr * row_stride + g * group_stride + lane * VW;
-  };
-  Raw nx[CH], ny[CH];
-  float nmean = 0.f, nrstd = 0.f;
-  auto fetch = [&](int r) {
-    if (r < a.R) {
-      const T *p = x + where(r, a.x_row, a.x_group), *q = dy + where(r, a.y_row, a.y_group);
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-        if (in[c]) {
-          nx[c] = *reinterpret_cast<const Raw *>(p + c * TPR * VW);
-          ny[c] = *reinterpret_cast<const Raw *>(q + c * TPR * VW);
-        }
-      nmean = a.mean[(long long)m * a.R + r];
-      nrstd = a.rstd[(long long)m * a.R + r];
+  int half = 0, slot = 0;
+  for (int r0 = blockIdx.x * RPB; r0 < a.R; r0 += step, r += step) {
+    float xh[CH][VW], g[CH][VW], s[2];
+    if constexpr (R::kStaged) {
+      fetch(r + (R::kDepth - 1) * step, slot == 0 ? R::kDepth - 1 : slot - 1);
+      ring.wait();
     }
-  };
-  const int step = gridDim.x * RPB;
-  int half = 0;
-  fetch(blockIdx.x * RPB + sub);
-  for (int r0 = blockIdx.x * RPB; r0 < a.R; r0 += step) {
-    const int r = r0 + sub;
-    float xh[CH][VW], g[CH][VW], s[2] = {0.f, 0.f};
     const float mean = nmean, rstd = nrstd;
+    if (r + step < a.R) nmean = a.mean[stat + r + step], nrstd = a.rstd[stat + r + step];
+    float s0[VW], s1[VW];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      unpack(nx[c], xh[c]);
-      unpack(ny[c], g[c]);
+    for (int j = 0; j < VW; ++j) s0[j] = s1[j] = 0.f;
 #pragma unroll
-      for (int j = 0; j < VW; ++j) {
-        if (!in[c] || r >= a.R) {
-          xh[c][j] = g[c][j] = 0.f;
-        } else {
-          xh[c][j] = (xh[c][j] - mean) * rstd;
-          dw[c][j] = fmaf(g[c][j], xh[c][j], dw[c][j]);
-          db[c][j] += g[c][j];
-          g[c][j] *= w[c][j];
-          s[0] += g[c][j];
-          s[1] = fmaf(g[c][j], xh[c][j], s[1]);
-        }
+    for (int c = 0; c < CH; ++c) { // where nothing is, dy reads as 0 and so does its product with a finite xh
+      const bool there = in[c] && r < a.R;
+      ring.read(slot, 0, c, xh[c], there);
+      ring.read(slot, 1, c, g[c], there);
+      if (there) {
+        E::add(xh[c], xh[c], -mean);
+        E::mul(xh[c], xh[c], rstd);
+        E::fma(dw[c], g[c], xh[c], dw[c]);
+        E::add(db[c], db[c], g[c]);
+        E::mul(g[c], g[c], w[c]);
+        E::add(s0, s0, g[c]);
+        E::fma(s1, g[c], xh[c], s1);
       }
     }
-    fetch(r + step);
+    if constexpr (!R::kStaged) fetch(r + step, 0);
+    slot = slot + 1 == R::kDepth ? 0 : slot + 1;
+    s[0] = E::sum(s0), s[1] = E::sum(s1);
     row_sum<TPR>(s, buf[half]);
     half ^= 1;
-    const float c1 = s[0] * inv_d, c2 = s[1] * inv_d;
     if (r < a.R) {
+      const float c1 = -s[0] * inv_d * rstd, c2 = -s[1] * inv_d * rstd; // dx = rstd g + c1 + xh c2
       T *p = dx + where(r, a.dx_row, a.dx_group);
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-#pragma unroll
-        for (int j = 0; j < VW; ++j) g[c][j] = rstd * (g[c][j] - c1 - xh[c][j] * c2);
+        E::fma(xh[c], xh[c], c2, c1);
+        E::fma(g[c], g[c], rstd, xh[c]);
         if (in[c]) store_vec<T, VW>(p + c * TPR * VW, g[c]);
       }
     }
@@ -279,7 +333,7 @@ template <typename T> __global__ void __launch_bounds__(kLoopThreads) norm_forwa
     }
     row_sum<kLoopThreads>(s, buf[half + 1]);
     half ^= 2;
-    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_d, a.eps));
+    const float rstd = rsqrtf(fmaf(s[0], inv_d, a.eps));
     for (int i = threadIdx.x; i < a.d; i += kLoopThreads) {
       load_vec<T, 1>(x + i, v);
       const float w = param_at(a.w, a.param_bf16, m * a.param_stride + i);
@@ -336,9 +390,9 @@ template <typename T> __global__ void __launch_bounds__(kLoopThreads) norm_backw
   }
 }
 
-// dweight, dbias [d] of every replica from the blocks' sums: 32 columns a block, the parts dealt to 16 rows of
+// dweight, dbias [d] of every replica from the blocks' sums: 32 columns a block, the parts dealt to 32 rows of
 // threads and joined in row order.
-constexpr int kJoinRows = 16;
+constexpr int kJoinRows = 32;
 __global__ void __launch_bounds__(32 * kJoinRows) norm_params_kernel(const float *part, int parts, int d, void *dw, void *db,
                                                                      long long grad_stride, int grad_bf16, int accumulate) {
   __shared__ float sums[kJoinRows][32];
@@ -376,14 +430,15 @@ struct Shape { // one register layout: vector width, threads per vector, accesse
   int vw, tpr, ch;
 };
 
-// The smallest layout that holds d elements.  A vector of at most 2 accesses per lane stays in one warp (no
-// barriers); longer ones take whole blocks.  Odd sizes and rows take single elements, 256 threads each.
+// The smallest layout that holds d elements, two accesses a thread where the vector has them (the steps of a sum over
+// the threads cost as much for one).  A vector of up to 64 accesses stays in one warp (no barriers); longer ones
+// take whole blocks.  Odd sizes and rows take single elements, 256 threads each.
 Shape shape_for(int d, int width, bool wide) {
   if (!wide) return d <= 1024 ? Shape{1, 256, 4} : d <= 4096 ? Shape{1, 256, 16} : Shape{0, SHAPE_LOOP, 0};
   const int n = d / width;
-  if (n <= 8) return {width, 8, 1};
-  if (n <= 16) return {width, 16, 1};
-  if (n <= 32) return {width, 32, 1};
+  if (n <= 8) return {width, 4, 2};
+  if (n <= 16) return {width, 8, 2};
+  if (n <= 32) return {width, 16, 2};
   if (n <= 64) return {width, 32, 2};
   if (n <= 128) return {width, 64, 2};
   if (n <= 256) return {width, 128, 2};
@@ -392,11 +447,12 @@ Shape shape_for(int d, int width, bool wide) {
   return {0, SHAPE_LOOP, 0};
 }
 
-// Blocks of a kernel that an SM holds at once, asked once.  Grids are that many: what goes beyond runs as a second,
+// Blocks of a kernel that an SM holds at once.  Grids are that many: what goes beyond runs as a second,
 // thinner wave.
-template <typename K> int ask_resident(K kernel, int threads) {
+template <typename K> int ask_resident(K kernel, int threads, int smem) {
   int n = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) != cudaSuccess) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess) {
     cudaGetLastError();
     n = 0;
   }
@@ -405,16 +461,17 @@ template <typename K> int ask_resident(K kernel, int threads) {
 
 template <typename T, int VW, int TPR, int CH> struct Kernels {
   static constexpr int kThreads = Block<TPR>::kThreads, kVectors = kThreads / TPR; // vectors of a block at a time
+  static constexpr int kForward = Ring<T, VW, TPR, CH, 1>::kBytes, kBackward = Ring<T, VW, TPR, CH, 2>::kBytes;
   static int forward_resident() {
-    static const int n = ask_resident(norm_forward_kernel<T, VW, TPR, CH>, kThreads);
-    return n;
+    static OncePerDevice once;
+    return once.get([] { return ask_resident(norm_forward_kernel<T, VW, TPR, CH>, kThreads, kForward); });
   }
   static int backward_resident() {
-    static const int n = ask_resident(norm_backward_kernel<T, VW, TPR, CH>, kThreads);
-    return n;
+    static OncePerDevice once;
+    return once.get([] { return ask_resident(norm_backward_kernel<T, VW, TPR, CH>, kThreads, kBackward); });
   }
-  static void forward(dim3 grid, cudaStream_t s, const NormArgs &a) { norm_forward_kernel<T, VW, TPR, CH><<<grid, kThreads, 0, s>>>(a); }
-  static void backward(dim3 grid, cudaStream_t s, const NormArgs &a) { norm_backward_kernel<T, VW, TPR, CH><<<grid, kThreads, 0, s>>>(a); }
+  static void forward(dim3 grid, cudaStream_t s, const NormArgs &a) { norm_forward_kernel<T, VW, TPR, CH><<<grid, kThreads, kForward, s>>>(a); }
+  static void backward(dim3 grid, cudaStream_t s, const NormArgs &a) { norm_backward_kernel<T, VW, TPR, CH><<<grid, kThreads, kBackward, s>>>(a); }
 };
 template <typename T> struct LoopKernels {
   static constexpr int kThreads = kLoopThreads, kVectors = 1;
@@ -428,9 +485,9 @@ template <typename T, typename F> auto with_shape_of(const Shape &s, F f) {
   constexpr int W = 16 / (int)sizeof(T);
 #define DILOCO_NORM_SHAPE(VW_, TPR_, CH_) \
   if (s.vw == VW_ && s.tpr == TPR_ && s.ch == CH_) return f(Kernels<T, VW_, TPR_, CH_>{});
-  DILOCO_NORM_SHAPE(W, 8, 1)
-  DILOCO_NORM_SHAPE(W, 16, 1)
-  DILOCO_NORM_SHAPE(W, 32, 1)
+  DILOCO_NORM_SHAPE(W, 4, 2)
+  DILOCO_NORM_SHAPE(W, 8, 2)
+  DILOCO_NORM_SHAPE(W, 16, 2)
   DILOCO_NORM_SHAPE(W, 32, 2)
   DILOCO_NORM_SHAPE(W, 64, 2)
   DILOCO_NORM_SHAPE(W, 128, 2)
@@ -457,7 +514,7 @@ int valid(const diloco_layernorm_t *n, bool backward) {
   if (backward) {
     if (!dtype_ok(n->grad_dtype) || n->dx_row_stride < 0 || n->dx_group_stride < 0) return DILOCO_ERR_INVALID_ARG;
   }
-  if (n->M > 65535 || n->d > 65536 || n->rows > INT32_MAX / n->groups) return DILOCO_ERR_UNSUPPORTED;
+  if (n->M > 65535 || n->d > 65536 || n->rows > (1 << 30) / n->groups) return DILOCO_ERR_UNSUPPORTED;
   return DILOCO_OK;
 }
 
@@ -472,6 +529,18 @@ int blocks_for(int R, int M, int per_block, int per_sm, int sms, int least) {
 int backward_blocks(const diloco_layernorm_t *n, int sms, bool wide) {
   const int R = (int)(n->rows * n->groups);
   return with_shape(n, wide, [&](auto k) { return blocks_for(R, n->M, k.kVectors, k.backward_resident(), sms, 4); });
+}
+
+// Division by `groups` as a multiplication: with s = ceil(log2 groups), magic = floor(2^32 (2^s - groups) / groups) + 2^32 + 1
+// would need 33 bits; for r < 2^31 one bit less is enough: magic = ceil(2^(31 + s) / groups) < 2^32, shift = s - 1.
+void set_groups(NormArgs &a, int groups) {
+  int s = 0;
+  while ((1 << s) < groups) ++s;
+  a.groups = groups;
+  if (groups > 1) {
+    a.magic = (unsigned)(((1ull << (31 + s)) + groups - 1) / groups);
+    a.shift = s - 1;
+  }
 }
 
 int current_sms(int *sms) {
@@ -504,7 +573,7 @@ int diloco_layernorm_forward(const diloco_layernorm_t *n, const void *x, const v
   NormArgs a = {};
   a.x = x, a.w = weight, a.b = bias, a.y = y, a.mean = mean, a.rstd = rstd;
   a.x_row = n->x_row_stride, a.x_group = n->x_group_stride, a.y_row = n->y_row_stride, a.y_group = n->y_group_stride;
-  a.param_stride = n->param_stride, a.R = R, a.groups = n->groups, a.d = n->d, a.eps = n->eps;
+  a.param_stride = n->param_stride, a.R = R, set_groups(a, n->groups), a.d = n->d, a.eps = n->eps;
   a.param_bf16 = n->param_dtype == DILOCO_DTYPE_BF16;
   const int width = (int)(16 / ea);
   const bool wide = aligned_to(x, 16) && aligned_to(y, 16) && n->d % width == 0 && multiple(a.x_row, a.x_group, width) &&
@@ -543,7 +612,7 @@ int diloco_layernorm_backward(const diloco_layernorm_t *n, const void *dy, const
   a.x = x, a.dy = dy, a.w = weight, a.dx = dx, a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
   a.x_row = n->x_row_stride, a.x_group = n->x_group_stride, a.y_row = n->y_row_stride, a.y_group = n->y_group_stride;
   a.dx_row = n->dx_row_stride, a.dx_group = n->dx_group_stride;
-  a.param_stride = n->param_stride, a.R = R, a.groups = n->groups, a.d = n->d, a.eps = n->eps;
+  a.param_stride = n->param_stride, a.R = R, set_groups(a, n->groups), a.d = n->d, a.eps = n->eps;
   a.param_bf16 = n->param_dtype == DILOCO_DTYPE_BF16, a.want_params = want, a.part = static_cast<float *>(workspace);
   const bool wide = aligned_to(x, 16) && aligned_to(dy, 16) && aligned_to(dx, 16) && n->d % width == 0 &&
                     multiple(a.x_row, a.x_group, width) && multiple(a.y_row, a.y_group, width) && multiple(a.dx_row, a.dx_group, width);

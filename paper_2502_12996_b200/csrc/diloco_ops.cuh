@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/diloco.h"
 
 namespace diloco {
@@ -39,6 +41,25 @@ struct PointerCheck {
 inline int sm_count(int device) {
   int n = 0;
   return cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) == cudaSuccess && n > 0 ? n : 148;
+}
+
+// Something about a kernel that is asked or set once on each device (an attribute, its blocks on an SM): f() > 0, or 0
+// where it failed, which is then asked again.
+struct OncePerDevice {
+  std::atomic<int> of[64];
+  template <typename F> int get(F f) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return f();
+    int v = of[dev].load(std::memory_order_acquire);
+    if (v == 0) of[dev].store(v = f(), std::memory_order_release);
+    return v;
+  }
+};
+// Lets a kernel have `bytes` of dynamic shared memory: 1, or 0 where the device refuses.
+template <typename K> int allow_smem(K kernel, int bytes) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess) return 1;
+  cudaGetLastError();
+  return 0;
 }
 
 inline int launched() {
@@ -100,6 +121,69 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
   return *reinterpret_cast<float2 *>(&r);
 }
+
+// The same over N values, in pairs where N is even: d = a b + c, a + b, a b; a single value stands for N equal ones.
+template <int N> struct Each {
+  static __device__ __forceinline__ float at(const float (&a)[N], int i) { return a[i]; }
+  static __device__ __forceinline__ float at(const float &a, int) { return a; }
+  template <typename A, typename B, typename C> static __device__ __forceinline__ void fma(float (&d)[N], const A &a, const B &b, const C &c) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const float2 r = fma2(make_float2(at(a, i), at(a, i + 1)), make_float2(at(b, i), at(b, i + 1)), make_float2(at(c, i), at(c, i + 1)));
+        d[i] = r.x, d[i + 1] = r.y;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] = fmaf(at(a, i), at(b, i), at(c, i));
+    }
+  }
+  template <typename A, typename B> static __device__ __forceinline__ void add(float (&d)[N], const A &a, const B &b) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const float2 r = add2(make_float2(at(a, i), at(a, i + 1)), make_float2(at(b, i), at(b, i + 1)));
+        d[i] = r.x, d[i + 1] = r.y;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] = at(a, i) + at(b, i);
+    }
+  }
+  template <typename A, typename B> static __device__ __forceinline__ void mul(float (&d)[N], const A &a, const B &b) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const float2 r = mul2(make_float2(at(a, i), at(a, i + 1)), make_float2(at(b, i), at(b, i + 1)));
+        d[i] = r.x, d[i + 1] = r.y;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] = at(a, i) * at(b, i);
+    }
+  }
+  static __device__ __forceinline__ float sum(const float (&a)[N]) {
+    if constexpr (N == 8) {
+      const float2 u = add2(add2(make_float2(a[0], a[1]), make_float2(a[2], a[3])), add2(make_float2(a[4], a[5]), make_float2(a[6], a[7])));
+      return u.x + u.y;
+    } else if constexpr (N == 4) {
+      const float2 u = add2(make_float2(a[0], a[1]), make_float2(a[2], a[3]));
+      return u.x + u.y;
+    } else {
+      float s = a[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) s += a[i];
+      return s;
+    }
+  }
+};
+
+// 16 bytes to shared memory, complete when a wait for the thread's group of copies returns
+__device__ __forceinline__ void copy_async16(unsigned smem, const void *g) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(g) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N = 0> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // V consecutive elements as floats; one access of V * sizeof(T) bytes (at most 16).
 template <typename T, int V> struct Pack;
