@@ -14,7 +14,7 @@
 //   3 sums     the sorted tokens in chunks of C, whatever ids they hold (an even split for any distribution): rows
 //              are added in order in registers; a run of one id inside a chunk is finished and written, a run
 //              that crosses chunks leaves fp32 partial sums
-//   4 join     runs that cross chunks: partial sums in chunk order, written by the chunk where the run starts
+//   4 join     runs that cross chunks (the second launch lists them): partial sums in chunk order
 // Sums run in token order inside a chunk, then in chunk order: a fixed order for given ids.
 #include <type_traits>
 
@@ -39,7 +39,8 @@ struct EmbedArgs {
   uint2 *tile_sorted, *gathered, *sorted; // [tokens] {id, token}: tile by tile, bucket by bucket, in order
   unsigned *tile_off;          // [tiles, kBuckets + 1] first place of each bucket in a tile; last: its valid tokens
   unsigned *count, *start;     // [vocab] tokens of an id, their first place in `sorted`
-  unsigned *total;             // [1] valid tokens
+  unsigned *total, *run_count; // [1] valid tokens, runs that cross chunks
+  unsigned *runs;              // [chunks] ids of those runs, in any order
   float *part;                 // [chunks, 2, d] run that began before the chunk, run that goes on after it
   int tiles, chunks, C;
 };
@@ -95,6 +96,7 @@ __global__ void __launch_bounds__(kTileThreads) embed_tiles_kernel(const EmbedAr
   __shared__ unsigned warp_total[W];
   const int m = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int w = 0; w < W; ++w) hist[w][threadIdx.x] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.run_count[m] = 0;
   __syncthreads();
   const long long first = (long long)blockIdx.x * kTile + warp * (kTile / W);
   int id[ROUNDS], rank[ROUNDS];
@@ -240,6 +242,8 @@ __global__ void __launch_bounds__(256) embed_buckets_kernel(const EmbedArgs a) {
       a.count[v] = c;
       a.start[v] = base + at;
       cnt[i0 + tid] = at;
+      if (c > 1 && (base + at) / a.C != (base + at + c - 1) / a.C) // the list's order changes nothing: a run has its own row
+        a.runs[m * a.chunks + atomicAdd(&a.run_count[m], 1u)] = (unsigned)(b + (i0 + tid) * kBuckets);
     }
   }
   if (b == kBuckets - 1 && tid == 0) a.total[m] = base + n;
@@ -301,11 +305,45 @@ template <typename GT, int VW> __device__ __forceinline__ void put_row(const Emb
   store_wide<GT, VW>(p, acc);
 }
 
+// A thread's pieces of the rows that its chunk adds up, on their way: blocks of 4 tokens in a ring in shared memory, filled
+// by asynchronous copies that each thread reads back itself (single elements: in registers, one block at a time).  What is
+// in flight costs no registers: with 8 rows in registers two blocks fit an SM and 65536 rows of 4 KB took 142 us.
+constexpr int kGroup = 4;
+template <typename AT, int VW> struct Rows {
+  static constexpr int W = VW * (int)sizeof(AT) <= 16 ? VW : 16 / (int)sizeof(AT), U = VW / W; // an access, accesses of a row
+  static constexpr bool kStaged = W * sizeof(AT) == 16;
+  static constexpr int kDepth = kStaged ? (U == 1 ? 4 : 2) : 1;
+  static constexpr int kBytes = kStaged ? kDepth * kGroup * U * kWorkThreads * 16 : 0;
+  using Raw = typename Pack<AT, W>::raw;
+  Raw held[kStaged ? 1 : kGroup][kStaged ? 1 : U];
+  unsigned char *mine;
+  __device__ __forceinline__ explicit Rows(unsigned char *smem) : mine(smem + threadIdx.x * 16) {}
+  __device__ __forceinline__ void fetch(int slot, int k, const AT *row) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if constexpr (kStaged)
+        copy_async16((unsigned)__cvta_generic_to_shared(mine) + ((slot * kGroup + k) * U + u) * kWorkThreads * 16, row + u * W);
+      else
+        held[k][u] = *reinterpret_cast<const Raw *>(row + u * W);
+    }
+  }
+  __device__ __forceinline__ void add(int slot, int k, float (&acc)[VW]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[W];
+      if constexpr (kStaged) unpack(*reinterpret_cast<const Raw *>(mine + ((slot * kGroup + k) * U + u) * kWorkThreads * 16), v);
+      else unpack(held[k][u], v);
+#pragma unroll
+      for (int j = 0; j < W; ++j) acc[u * W + j] += v[j];
+    }
+  }
+};
+
 // Chunks, `lanes` threads each and VW columns a thread (blockIdx.z: further columns).
 template <typename AT, typename GT, int VW>
-__global__ void __launch_bounds__(kWorkThreads, 2) embed_sums_kernel(const EmbedArgs a, int lanes) {
-  constexpr int W = VW * (int)sizeof(AT) <= 16 ? VW : 16 / (int)sizeof(AT); // elements of one access
-  constexpr int ROWS = W == VW ? 8 : 4;                                      // tokens in flight
+__global__ void __launch_bounds__(kWorkThreads, 3) embed_sums_kernel(const EmbedArgs a, int lanes) {
+  using R = Rows<AT, VW>;
+  extern __shared__ __align__(16) unsigned char staged[];
   const int m = blockIdx.y, lane = threadIdx.x % lanes, worker = threadIdx.x / lanes, workers = kWorkThreads / lanes;
   const int col = (blockIdx.z * lanes + lane) * VW;
   grid_wait();
@@ -316,55 +354,58 @@ __global__ void __launch_bounds__(kWorkThreads, 2) embed_sums_kernel(const Embed
   const unsigned c0 = chunk < a.chunks ? (unsigned)(chunk * a.C) : total;
   if (c0 >= total) return; // whole warps: a worker is one warp or several
   const unsigned c1 = min(c0 + a.C, total);
+  const int n = (int)(c1 - c0);
   const bool in = col < a.d;
   float acc[VW];
 #pragma unroll
   for (int j = 0; j < VW; ++j) acc[j] = 0.f;
   float *part = a.part + ((long long)m * a.chunks + chunk) * 2 * a.d + col;
-  // lane l of a warp holds entry l of the next 32; the neighbours tell whether a run crosses the chunk's ends
+  // lane l of a warp holds entries base + l and base + 32 + l of the chunk; the neighbours tell whether a run crosses its ends
   const int wl = threadIdx.x & 31;
-  uint2 mine = c0 + wl < c1 ? sorted[c0 + wl] : make_uint2(0, 0);
+  auto entry = [&](int e) { return e < n ? sorted[c0 + e] : make_uint2(0, 0); };
+  uint2 now = entry(wl), then = entry(32 + wl);
+  int base = 0;
   const unsigned before = c0 > 0 ? sorted[c0 - 1].x : 0xffffffffu, after = c1 < total ? sorted[c1].x : 0xffffffffu;
-  unsigned cur = __shfl_sync(0xffffffffu, mine.x, 0);
+  unsigned cur = __shfl_sync(0xffffffffu, now.x, 0);
   bool began = before == cur;
-  for (unsigned e0 = c0; e0 < c1; e0 += 32) {
-    const uint2 held = mine;
-    if (e0 + 32 + wl < c1) mine = sorted[e0 + 32 + wl];
+  R rows(staged);
+  auto fetch = [&](int b) { // block b: at most 12 entries ahead of `base` + 32
 #pragma unroll
-    for (int b = 0; b < 32; b += ROWS) {
-      if (e0 + b >= c1) break; // the same for the whole warp
-      typename Pack<AT, W>::raw raw[ROWS][VW / W];
-      unsigned id[ROWS];
+    for (int k = 0; k < kGroup; ++k) {
+      const int e = b * kGroup + k, o = e - base;
+      const unsigned x = __shfl_sync(0xffffffffu, now.y, o & 31), y = __shfl_sync(0xffffffffu, then.y, o & 31);
+      if (e < n && in) rows.fetch(b % R::kDepth, k, dout + (long long)(o < 32 ? x : y) * a.row_stride);
+    }
+    if constexpr (R::kStaged) copy_commit();
+  };
+  const int blocks = (n + kGroup - 1) / kGroup;
 #pragma unroll
-      for (int k = 0; k < ROWS; ++k) {
-        id[k] = __shfl_sync(0xffffffffu, held.x, b + k);
-        const unsigned token = __shfl_sync(0xffffffffu, held.y, b + k);
-        if (in && e0 + b + k < c1)
+  for (int b = 0; b < R::kDepth - 1; ++b) fetch(b);
+  for (int b = 0; b < blocks; ++b) {
+    if (b * kGroup - base == 32) {
+      now = then;
+      base += 32;
+      then = entry(base + 32 + wl);
+    }
+    fetch(b + R::kDepth - 1);
+    if constexpr (R::kStaged) copy_wait<R::kDepth - 1>();
 #pragma unroll
-          for (int u = 0; u < VW / W; ++u)
-            raw[k][u] = *reinterpret_cast<const typename Pack<AT, W>::raw *>(dout + (long long)token * a.row_stride + u * W);
-      }
-#pragma unroll
-      for (int k = 0; k < ROWS; ++k)
-        if (e0 + b + k < c1) {
-          if (id[k] != cur) { // the same for every thread of the worker
-            if (in) {
-              if (began) store_wide<float, VW>(part, acc);
-              else put_row<GT, VW>(a, m, cur, col, acc);
-            }
-            began = false;
-            cur = id[k];
-#pragma unroll
-            for (int j = 0; j < VW; ++j) acc[j] = 0.f;
+    for (int k = 0; k < kGroup; ++k) {
+      const int e = b * kGroup + k;
+      const unsigned id = __shfl_sync(0xffffffffu, now.x, (e - base) & 31);
+      if (e < n) { // as id != cur, the same for every thread of the worker
+        if (id != cur) {
+          if (in) {
+            if (began) store_wide<float, VW>(part, acc);
+            else put_row<GT, VW>(a, m, cur, col, acc);
           }
+          began = false;
+          cur = id;
 #pragma unroll
-          for (int u = 0; u < VW / W; ++u) {
-            float v[W];
-            unpack(raw[k][u], v);
-#pragma unroll
-            for (int j = 0; j < W; ++j) acc[u * W + j] += v[j];
-          }
+          for (int j = 0; j < VW; ++j) acc[j] = 0.f;
         }
+        if (in) rows.add(b % R::kDepth, k, acc);
+      }
     }
   }
   if (!in) return;
@@ -373,34 +414,34 @@ __global__ void __launch_bounds__(kWorkThreads, 2) embed_sums_kernel(const Embed
   else put_row<GT, VW>(a, m, cur, col, acc);
 }
 
+// Runs that cross chunks: few of them, the commonest ids' long.  A warp takes one run's next 32 * VW columns and has BATCH
+// rows of partial sums in flight.
 template <typename GT, int VW>
-__global__ void __launch_bounds__(kWorkThreads) embed_join_kernel(const EmbedArgs a, int lanes) {
-  const int m = blockIdx.y, lane = threadIdx.x % lanes, worker = threadIdx.x / lanes, workers = kWorkThreads / lanes;
-  const int col = (blockIdx.z * lanes + lane) * VW;
+__global__ void __launch_bounds__(kWorkThreads, 4) embed_join_kernel(const EmbedArgs a) {
+  constexpr int BATCH = VW == 1 ? 16 : 8, WARPS = kWorkThreads / 32;
+  const int m = blockIdx.y, lane = threadIdx.x & 31, slabs = (a.d + 32 * VW - 1) / (32 * VW);
   grid_wait();
-  const long long chunk = (long long)blockIdx.x * workers + worker;
-  if (chunk >= a.chunks || col >= a.d) return;
-  const unsigned total = a.total[m];
-  const unsigned long long end = (unsigned long long)(chunk + 1) * a.C;
-  if (end >= total) return; // the last chunk's last run goes on nowhere
-  const unsigned id = a.sorted[m * a.tokens + end - 1].x;
-  const unsigned first = a.start[m * a.vocab + id], last = first + a.count[m * a.vocab + id] - 1;
-  if (first / a.C != chunk || last / a.C == chunk) return;
-  const float *part = a.part + (long long)m * a.chunks * 2 * a.d + col;
-  float acc[VW];
-  load_wide<float, VW>(part + (chunk * 2 + 1) * a.d, acc);
-  const long long to = last / a.C;
-  constexpr int BATCH = 8; // partial sums in flight: the commonest id of a text has one in every few chunks
-  for (long long c = chunk + 1; c <= to; c += BATCH) {
-    float v[BATCH][VW];
+  const long long items = (long long)a.run_count[m] * slabs;
+  for (long long i = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5); i < items; i += (long long)gridDim.x * WARPS) {
+    const unsigned id = a.runs[m * a.chunks + i / slabs];
+    const int col = ((int)(i % slabs) * 32 + lane) * VW;
+    const unsigned first = a.start[m * a.vocab + id], last = first + a.count[m * a.vocab + id] - 1;
+    if (col >= a.d) continue;
+    const long long from = first / a.C, to = last / a.C;
+    const float *part = a.part + (long long)m * a.chunks * 2 * a.d + col;
+    float acc[VW];
+    load_wide<float, VW>(part + (from * 2 + 1) * a.d, acc);
+    for (long long c = from + 1; c <= to; c += BATCH) {
+      float v[BATCH][VW];
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k)
-      if (c + k <= to) load_wide<float, VW>(part + (c + k) * 2 * a.d, v[k]);
+      for (int k = 0; k < BATCH; ++k)
+        if (c + k <= to) load_wide<float, VW>(part + (c + k) * 2 * a.d, v[k]);
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k)
-      if (c + k <= to) Each<VW>::add(acc, acc, v[k]);
+      for (int k = 0; k < BATCH; ++k)
+        if (c + k <= to) Each<VW>::add(acc, acc, v[k]);
+    }
+    put_row<GT, VW>(a, m, id, col, acc);
   }
-  put_row<GT, VW>(a, m, id, col, acc);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -422,16 +463,17 @@ int lanes_for(int d, int vw) {
   return lanes;
 }
 
-// Tokens of one chunk: 32, more where that would give each SM over 64 chunks (its partial rows would cost more
-// than the finer split brings).
+// Tokens of one chunk: 32, twice as many (up to 256) as long as the SMs still get two rounds of chunks: every run that crosses
+// chunks costs the join a chain of loads, and every chunk up to two rows of partial sums.
 int chunk_for(const diloco_embedding_t *e) {
+  const int64_t lanes = lanes_for(e->d, 8), round = 148 * 3 * kWorkThreads; // threads of a round, three blocks an SM
   int c = 32;
-  while (c < 256 && e->tokens * e->M / c > 148 * 64) c *= 2;
+  while (c < 256 && e->tokens * e->M * lanes / (2 * c) >= 2 * round) c *= 2;
   return c;
 }
 
 struct Layout {
-  int64_t tile_sorted, gathered, sorted, tile_off, count, start, total, part, bytes;
+  int64_t tile_sorted, gathered, sorted, tile_off, count, start, total, run_count, runs, part, bytes;
   int tiles, chunks, C;
 };
 Layout layout(const diloco_embedding_t *e) {
@@ -452,6 +494,8 @@ Layout layout(const diloco_embedding_t *e) {
   l.count = take(4 * e->M * e->vocab);
   l.start = take(4 * e->M * e->vocab);
   l.total = take(4 * e->M);
+  l.run_count = take(4 * e->M);
+  l.runs = take(4ll * e->M * l.chunks);
   l.part = take(4ll * e->M * l.chunks * 2 * e->d);
   l.bytes = at;
   return l;
@@ -528,7 +572,8 @@ int diloco_embedding_backward(const diloco_embedding_t *e, const void *ids, cons
   a.tile_sorted = reinterpret_cast<uint2 *>(ws + l.tile_sorted), a.gathered = reinterpret_cast<uint2 *>(ws + l.gathered);
   a.sorted = reinterpret_cast<uint2 *>(ws + l.sorted), a.tile_off = reinterpret_cast<unsigned *>(ws + l.tile_off);
   a.count = reinterpret_cast<unsigned *>(ws + l.count), a.start = reinterpret_cast<unsigned *>(ws + l.start);
-  a.total = reinterpret_cast<unsigned *>(ws + l.total), a.part = reinterpret_cast<float *>(ws + l.part);
+  a.total = reinterpret_cast<unsigned *>(ws + l.total), a.run_count = reinterpret_cast<unsigned *>(ws + l.run_count);
+  a.runs = reinterpret_cast<unsigned *>(ws + l.runs), a.part = reinterpret_cast<float *>(ws + l.part);
   a.tiles = l.tiles, a.chunks = l.chunks, a.C = l.C;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (l.tiles) {
@@ -545,9 +590,20 @@ int diloco_embedding_backward(const diloco_embedding_t *e, const void *ids, cons
     const int slabs = (e->d + lanes * w.value - 1) / (lanes * w.value);
     const int sums = (l.chunks + workers - 1) / workers;
     if (sums == 0) return;
-    rc = launch_chained(embed_sums_kernel<decltype(t), decltype(g), w.value>, dim3(sums, e->M, slabs), dim3(kWorkThreads), 0, st, a, lanes);
+    const auto kernel = embed_sums_kernel<decltype(t), decltype(g), w.value>;
+    constexpr int bytes = Rows<decltype(t), w.value>::kBytes;
+    static OncePerDevice once;
+    if (!once.get([&] { return allow_smem(kernel, bytes); })) {
+      rc = DILOCO_ERR_CUDA;
+      return;
+    }
+    rc = launch_chained(kernel, dim3(sums, e->M, slabs), dim3(kWorkThreads), bytes, st, a, lanes);
     if (rc != DILOCO_OK || l.chunks < 2) return;
-    rc = launch_chained(embed_join_kernel<decltype(g), w.value>, dim3(sums, e->M, slabs), dim3(kWorkThreads), 0, st, a, lanes);
+    constexpr int JW = w.value < 4 ? w.value : 4;
+    // at most one run for each chunk
+    const int64_t items = (int64_t)l.chunks * ((e->d + 32 * JW - 1) / (32 * JW)), warps = kWorkThreads / 32;
+    const int64_t want = (items + warps - 1) / warps, most = (4ll * sm_count(pc.device) + e->M - 1) / e->M;
+    rc = launch_chained(embed_join_kernel<decltype(g), JW>, dim3((unsigned)(want < most ? want : most), e->M), dim3(kWorkThreads), 0, st, a);
   });
   return rc;
 }
