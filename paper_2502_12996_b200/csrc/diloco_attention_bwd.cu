@@ -14,7 +14,8 @@
 // are 128 x 128; warps 0-3 take the first 64 columns, warps 4-7 the last, one row a thread.  Rows of a partial last
 // tile are zeroed in shared memory where they are summed over; a row that comes out non-finite is computed
 // again over the rows it has to do with alone.
-#include "diloco_attention_rows.cuh"
+#include <type_traits>
+
 #include "diloco_attention_tiles.cuh"
 
 namespace diloco {
@@ -210,7 +211,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int j = 0; j < 32; ++j) s[u][j] = __float_as_uint(ex2(fmaf(__uint_as_float(s[u][j]), c, -lse2)));
+        for (int j = 0; j < 32; j += 2) {
+          const float2 y = fma2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), make_float2(c, c), make_float2(-lse2, -lse2));
+          s[u][j] = __float_as_uint(ex2(y.x)), s[u][j + 1] = __float_as_uint(ex2(y.y));
+        }
       if (it == 0) { // the diagonal tile is the last of the sequence's that this block sees
         const int valid = at.end - q0; // K rows of it inside the sequence
         if (valid < kRows) {
@@ -223,21 +227,27 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       ok = warp_wait(&bar.dp_full, it & 1, &bar.abort);
       if (!ok) break;
       tmem_fence_after();
+      auto slopes = [&](auto masked) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        unsigned d[32], x[16];
-        tmem_load32(t_dp + half * 64 + u * 32 + lanes, d);
-        tmem_wait_load();
+        for (int u = 0; u < 2; ++u) {
+          unsigned d[32], x[16];
+          tmem_load32(t_dp + half * 64 + u * 32 + lanes, d);
+          tmem_wait_load();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          float v = __uint_as_float(s[u][j]) * (__uint_as_float(d[j]) - delta);
-          if (it == 0 && half * 64 + u * 32 + j > r) v = 0.f;
-          d[j] = __float_as_uint(v);
+          for (int j = 0; j < 32; j += 2) {
+            float2 y = add2(make_float2(__uint_as_float(d[j]), __uint_as_float(d[j + 1])), make_float2(-delta, -delta));
+            y = mul2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), y);
+            if (decltype(masked)::value) {
+              if (half * 64 + u * 32 + j > r) y.x = 0.f;
+              if (half * 64 + u * 32 + j + 1 > r) y.y = 0.f;
+            }
+            x[j / 2] = bf16_pair(y.x, y.y);
+          }
+          tmem_store16(t_dp + half * 64 + u * 16 + lanes, x);
         }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = bf16_pair(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1]));
-        tmem_store16(t_dp + half * 64 + u * 16 + lanes, x);
-      }
+      };
+      if (it == 0) slopes(std::true_type{});
+      else slopes(std::false_type{});
       tmem_wait_store();
       tmem_fence_before();
       mbar_arrive(&bar.ds_full);
@@ -296,7 +306,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   const int per_head = (at.end - k0 + kRows - 1) / kRows, tiles = per_head * a.group; // query tiles
   const unsigned smem = (smem_u32(raw_smem) + 1023) & ~1023u;
   const unsigned s_k = smem + L::kOwn, s_v = s_k + L::kTileBytes, s_q = smem + L::kRing, s_do = s_q + kStages * L::kTileBytes;
-  // log-sum-exp (times log2 e) and delta of a query tile's rows
+  // minus log-sum-exp (times log2 e) and minus delta of a query tile's rows
   float *stats = reinterpret_cast<float *>(raw_smem + (smem - smem_u32(raw_smem)) + L::kStats);
 
   if (warp == 8) tmem_alloc(&bar.tmem, 512);
@@ -342,8 +352,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
           const int i = row + u * 32 + lane;
           const bool in = i < at.end;
           const long long stat = (long long)h * a.tokens + i;
-          to[u * 32 + lane] = in ? a.lse[stat] * kLog2e : 0.f;
-          to[kRows + u * 32 + lane] = in ? a.delta[stat] : 0.f;
+          to[u * 32 + lane] = in ? -a.lse[stat] * kLog2e : 0.f;
+          to[kRows + u * 32 + lane] = in ? -a.delta[stat] : 0.f;
         }
         mbar_arrive(&bar.stat_full[s]);
       }
@@ -412,27 +422,33 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       if (!ok) break;
       const float4 *lse = reinterpret_cast<const float4 *>(stats + st * 2 * kRows + half * 64);
       const float4 *delta = lse + kRows / 4;
+      // query q sees this key from the diagonal on, and there are `valid` queries: masks on the edge tiles alone
+      auto hidden = [&](int u, int j) {
+        const int q = half * 64 + u * 32 + j;
+        return (t == 0 && q < r) || q >= valid;
+      };
+      auto weights = [&](auto masked) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        unsigned x[16];
+        for (int u = 0; u < 2; ++u) {
+          unsigned x[16];
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-          const float4 m = lse[u * 8 + j / 4];
-          const float ml[4] = {m.x, m.y, m.z, m.w};
+          for (int j = 0; j < 32; j += 4) {
+            const float4 m = lse[u * 8 + j / 4];
+            const float2 y[2] = {fma2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), make_float2(c, c), make_float2(m.x, m.y)),
+                                 fma2(make_float2(__uint_as_float(s[u][j + 2]), __uint_as_float(s[u][j + 3])), make_float2(c, c), make_float2(m.z, m.w))};
+            float p[4] = {ex2(y[0].x), ex2(y[0].y), ex2(y[1].x), ex2(y[1].y)};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float p = ex2(fmaf(__uint_as_float(s[u][j + e]), c, -ml[e]));
-            if (edge) { // query q sees this key from the diagonal on, and there are `valid` queries
-              const int q = half * 64 + u * 32 + j + e;
-              if ((t == 0 && q < r) || q >= valid) p = 0.f;
+            for (int e = 0; e < 4; ++e) {
+              if (decltype(masked)::value && hidden(u, j + e)) p[e] = 0.f;
+              s[u][j + e] = __float_as_uint(p[e]);
             }
-            s[u][j + e] = __float_as_uint(p);
+            x[j / 2] = bf16_pair(p[0], p[1]), x[j / 2 + 1] = bf16_pair(p[2], p[3]);
           }
+          tmem_store16(t_s + half * 64 + u * 16 + lanes, x);
         }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = bf16_pair(__uint_as_float(s[u][2 * j]), __uint_as_float(s[u][2 * j + 1]));
-        tmem_store16(t_s + half * 64 + u * 16 + lanes, x);
-      }
+      };
+      if (edge) weights(std::true_type{});
+      else weights(std::false_type{});
       if (valid < kRows) {
         ok = warp_wait(&bar.q_full[st], ph, &bar.abort) && warp_wait(&bar.do_full[st], ph, &bar.abort);
         if (!ok) break;
@@ -449,29 +465,32 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       ok = warp_wait(&bar.dp_full, it & 1, &bar.abort);
       if (!ok) break;
       tmem_fence_after();
+      auto slopes = [&](auto masked) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        unsigned d[32], x[16];
-        tmem_load32(t_dp + half * 64 + u * 32 + lanes, d);
-        tmem_wait_load();
+        for (int u = 0; u < 2; ++u) {
+          unsigned d[32], x[16];
+          tmem_load32(t_dp + half * 64 + u * 32 + lanes, d);
+          tmem_wait_load();
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-          const float4 m = delta[u * 8 + j / 4];
-          const float dl[4] = {m.x, m.y, m.z, m.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float v = __uint_as_float(s[u][j + e]) * (__uint_as_float(d[j + e]) - dl[e]);
-            if (edge) {
-              const int q = half * 64 + u * 32 + j + e;
-              if ((t == 0 && q < r) || q >= valid) v = 0.f;
+          for (int j = 0; j < 32; j += 4) {
+            const float4 m = delta[u * 8 + j / 4];
+            float2 y[2] = {add2(make_float2(__uint_as_float(d[j]), __uint_as_float(d[j + 1])), make_float2(m.x, m.y)),
+                           add2(make_float2(__uint_as_float(d[j + 2]), __uint_as_float(d[j + 3])), make_float2(m.z, m.w))};
+            y[0] = mul2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), y[0]);
+            y[1] = mul2(make_float2(__uint_as_float(s[u][j + 2]), __uint_as_float(s[u][j + 3])), y[1]);
+            if (decltype(masked)::value) { // 0 * (infinity or NaN of a row that is not seen)
+              if (hidden(u, j)) y[0].x = 0.f;
+              if (hidden(u, j + 1)) y[0].y = 0.f;
+              if (hidden(u, j + 2)) y[1].x = 0.f;
+              if (hidden(u, j + 3)) y[1].y = 0.f;
             }
-            d[j + e] = __float_as_uint(v);
+            x[j / 2] = bf16_pair(y[0].x, y[0].y), x[j / 2 + 1] = bf16_pair(y[1].x, y[1].y);
           }
+          tmem_store16(t_dp + half * 64 + u * 16 + lanes, x);
         }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = bf16_pair(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1]));
-        tmem_store16(t_dp + half * 64 + u * 16 + lanes, x);
-      }
+      };
+      if (edge) slopes(std::true_type{});
+      else slopes(std::false_type{});
       tmem_wait_store();
       tmem_fence_before();
       mbar_arrive(&bar.ds_full);

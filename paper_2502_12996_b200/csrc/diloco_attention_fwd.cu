@@ -15,6 +15,8 @@
 // Tiles of a sequence that start together on both axes need a mask on the diagonal tile alone.  V rows behind the
 // sequence's end are zeroed in shared memory (0 * NaN); a row that comes out non-finite all the same is computed
 // again over the rows that it sees alone, so that a later token's NaN cannot reach an earlier one.
+#include <type_traits>
+
 #include "diloco_attention_tiles.cuh"
 
 namespace diloco {
@@ -176,11 +178,12 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
         float top[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          top[i] = __uint_as_float(s[i][0]);
+          top[i] = max3(__uint_as_float(s[i][0]), __uint_as_float(s[i][1]), __uint_as_float(s[i][2]));
 #pragma unroll
-          for (int j = 1; j < 32; ++j) top[i] = fmaxf(top[i], __uint_as_float(s[i][j]));
+          for (int j = 3; j < 31; j += 2) top[i] = max3(top[i], __uint_as_float(s[i][j]), __uint_as_float(s[i][j + 1]));
+          top[i] = fmaxf(top[i], __uint_as_float(s[i][31]));
         }
-        const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const float mt = fmaxf(max3(top[0], top[1], top[2]), top[3]);
         if (n == 0) m = mt;
         else {
           const bool grew = (mt - m) * c > 8.f;
@@ -199,24 +202,30 @@ __global__ void __launch_bounds__(kFwdThreads, 1)
             }
           }
         }
-        const float mc = m * c;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const float2 mc = make_float2(-m * c, -m * c), cc = make_float2(c, c);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        auto weights = [&](auto masked) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          unsigned p[16];
+          for (int i = 0; i < 4; ++i) {
+            unsigned p[16];
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            float x = ex2(fmaf(__uint_as_float(s[i][j]), c, -mc)), y = ex2(fmaf(__uint_as_float(s[i][j + 1]), c, -mc));
-            if (n == 0) { // scale = 0 leaves no -infinity in the masked places
-              if (i * 32 + j > r) x = 0.f;
-              if (i * 32 + j + 1 > r) y = 0.f;
+            for (int j = 0; j < 32; j += 2) {
+              const float2 y = fma2(make_float2(__uint_as_float(s[i][j]), __uint_as_float(s[i][j + 1])), cc, mc);
+              float2 x = make_float2(ex2(y.x), ex2(y.y));
+              if (decltype(masked)::value) { // scale = 0 leaves no -infinity in the masked places
+                if (i * 32 + j > r) x.x = 0.f;
+                if (i * 32 + j + 1 > r) x.y = 0.f;
+              }
+              sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], x);
+              p[j / 2] = bf16_pair(x.x, x.y);
             }
-            sum[(j >> 1) & 3] += x + y;
-            p[j / 2] = bf16_pair(x, y);
+            tmem_store16(ts + i * 16, p);
           }
-          tmem_store16(ts + i * 16, p);
-        }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        };
+        if (n == 0) weights(std::true_type{});
+        else weights(std::false_type{});
+        sum[0] = add2(sum[0], sum[1]);
+        l += sum[0].x + sum[0].y;
         if (n == 0) {
           const int valid = at.end - (q0 + w * kRows); // V rows of this tile inside the sequence
           if (valid < kRows) {
