@@ -22,8 +22,6 @@ namespace diloco {
 namespace {
 
 constexpr int kBwdThreads = 384;
-// launched with 168 registers a thread (64512 of a block): 2 x 128 x 208 + 128 x 88 = 64512
-constexpr int kMathRegs = 208, kOtherRegs = 88;
 constexpr int kStages = 2;
 
 template <int HD> struct BwdLayout { // two tiles of the block's own, two rings
@@ -34,34 +32,6 @@ template <int HD> struct BwdLayout { // two tiles of the block's own, two rings
 };
 
 __device__ __forceinline__ void math_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
-// One row's half of an accumulator (columns c0 to c1 of a tile of HD) times `factor` to bf16; whether all of it is finite.
-template <int N> __device__ __forceinline__ bool put_half_row(unsigned tmem, __nv_bfloat16 *row, int c0, int head_dim, float factor, bool mine) {
-  bool fine = true;
-#pragma unroll
-  for (int i = 0; i < N; i += 32) {
-    unsigned o[32];
-    tmem_load32(tmem + c0 + i, o);
-    tmem_wait_load();
-    float v[32];
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      v[j] = __uint_as_float(o[j]) * factor;
-      fine &= fabsf(v[j]) < INFINITY;
-    }
-    if (mine) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (c0 + i + u * 8 < head_dim) {
-          uint4 x;
-          x.x = bf16_pair(v[u * 8], v[u * 8 + 1]), x.y = bf16_pair(v[u * 8 + 2], v[u * 8 + 3]);
-          x.z = bf16_pair(v[u * 8 + 4], v[u * 8 + 5]), x.w = bf16_pair(v[u * 8 + 6], v[u * 8 + 7]);
-          *reinterpret_cast<uint4 *>(row + c0 + i + u * 8) = x;
-        }
-    }
-  }
-  return fine;
-}
 
 // ------------------------------------------------------------------------------------- dq
 struct DqBarriers {
@@ -75,14 +45,15 @@ struct DqBarriers {
 template <int HD>
 __global__ void __launch_bounds__(kBwdThreads, 1)
     attn_dq_kernel(const AttnArgs a, const __grid_constant__ HeadMap mq, const __grid_constant__ HeadMap mk, const __grid_constant__ HeadMap mv,
-                   const __grid_constant__ HeadMap mdo, int slots) {
+                   const __grid_constant__ HeadMap mdo, int split) {
   using L = BwdLayout<HD>;
   extern __shared__ unsigned char raw_smem[];
   __shared__ DqBarriers bar;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int h = blockIdx.x % a.heads, g = h / a.group;
-  const Place at = place_of(a, slots - 1 - (int)(blockIdx.x / a.heads), kRows);
+  const int part = cluster_rank(), unit = blockIdx.x / split, h = unit % a.heads, g = h / a.group;
+  const Place at = place_of<false>(a, unit / a.heads, kRows);
   if (at.block < 0) {
+    if (part != 0) return;
     const int r0 = at.first + (-1 - at.block) * kRows;
     for (int r = r0 + warp; r < min(r0 + kRows, at.end); r += kBwdThreads / 32) {
       for (int c = lane; c < a.head_dim; c += 32) a.dq[r * a.dq_row + h * a.dq_head + c] = __float2bfloat16_rn(0.f);
@@ -91,7 +62,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   }
   const int q0 = at.first + at.block * kRows;
   if (q0 >= at.end) return;
-  const int tiles = at.block + 1;
+  const int all = at.block + 1, tiles = (all - part + split - 1) / split; // this block's key tiles: part, part + split, ...
   const unsigned smem = (smem_u32(raw_smem) + 1023) & ~1023u;
   const unsigned s_q = smem + L::kOwn, s_do = s_q + L::kTileBytes, s_k = smem + L::kRing, s_v = s_k + kStages * L::kTileBytes;
 
@@ -112,14 +83,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   const unsigned tmem = bar.tmem, t_s = tmem, t_dp = tmem + 256, t_dq = tmem + 384;
 
   if (warp >= 8) {
-    registers_down<kOtherRegs>();
     if (warp == 9 && lane == 0) {
       int issued = 0;
-      mbar_expect_tx(&bar.own_full, 2 * L::kTileBytes);
-      load_tile<HD>(s_q, mq, h, q0, &bar.own_full);
-      load_tile<HD>(s_do, mdo, h, q0, &bar.own_full);
+      if (tiles > 0) {
+        mbar_expect_tx(&bar.own_full, 2 * L::kTileBytes);
+        load_tile<HD>(s_q, mq, h, q0, &bar.own_full);
+        load_tile<HD>(s_do, mdo, h, q0, &bar.own_full);
+      }
       for (int it = 0; it < tiles; ++it) {
-        const int s = it % kStages, row = at.first + (tiles - 1 - it) * kRows;
+        const int s = it % kStages, row = at.first + (all - 1 - (it * split + part)) * kRows;
         const unsigned ph = ((it / kStages) & 1) ^ 1;
         if (!wait_or_abort(&bar.k_empty[s], ph, &bar.abort)) break;
         mbar_expect_tx(&bar.k_full[s], L::kTileBytes);
@@ -131,7 +103,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         issued = 2 * it + 2;
       }
       if (issued < 2 * tiles) land_copies<kStages>(issued, &bar.own_full, bar.k_full, bar.v_full);
-    } else if (warp == 8 && lane == 0) {
+    } else if (warp == 8 && lane == 0 && tiles > 0) {
       constexpr unsigned kk = mma_desc(128, false, false), kn = mma_desc(HD, false, true);
       bool ok = wait_or_abort(&bar.own_full, 0, &bar.abort) && wait_or_abort(&bar.k_full[0], 0, &bar.abort);
       if (ok) {
@@ -170,8 +142,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         }
       }
     }
+    __syncwarp();
+    if (split > 1) {
+      cluster_sync();
+      cluster_sync();
+    }
   } else {
-    registers_up<kMathRegs>();
     const int half = warp >> 2, r = threadIdx.x & 127, i = q0 + r;
     const bool mine = i < at.end;
     const unsigned lanes = (unsigned)(warp & 3) << 21;
@@ -196,7 +172,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     math_sync();
     delta = bar.delta[0][r] + bar.delta[1][r];
     const long long stat = (long long)h * a.tokens + i;
-    if (mine && half == 0) a.delta[stat] = delta;
+    if (mine && half == 0 && part == 0) a.delta[stat] = delta;
     const float lse2 = mine ? a.lse[stat] * kLog2e : 0.f;
     const float c = a.scale_log2;
     bool ok = true;
@@ -215,7 +191,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
           const float2 y = fma2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), make_float2(c, c), make_float2(-lse2, -lse2));
           s[u][j] = __float_as_uint(ex2(y.x)), s[u][j + 1] = __float_as_uint(ex2(y.y));
         }
-      if (it == 0) { // the diagonal tile is the last of the sequence's that this block sees
+      const bool diagonal = it == 0 && part == 0;
+      if (diagonal) { // it is the last of the sequence's tiles that this block sees
         const int valid = at.end - q0; // K rows of it inside the sequence
         if (valid < kRows) {
           ok = warp_wait(&bar.k_full[0], 0, &bar.abort);
@@ -230,7 +207,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       auto slopes = [&](auto masked) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          unsigned d[32], x[16];
+          unsigned d[32], x[8];
           tmem_load32(t_dp + half * 64 + u * 32 + lanes, d);
           tmem_wait_load();
 #pragma unroll
@@ -241,25 +218,45 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
               if (half * 64 + u * 32 + j > r) y.x = 0.f;
               if (half * 64 + u * 32 + j + 1 > r) y.y = 0.f;
             }
-            x[j / 2] = bf16_pair(y.x, y.y);
+            x[j / 2 % 8] = bf16_pair(y.x, y.y);
+            if (j % 16 == 14) tmem_store8(t_dp + half * 64 + u * 16 + j / 16 * 8 + lanes, x);
           }
-          tmem_store16(t_dp + half * 64 + u * 16 + lanes, x);
         }
       };
-      if (it == 0) slopes(std::true_type{});
+      if (diagonal) slopes(std::true_type{});
       else slopes(std::false_type{});
       tmem_wait_store();
       tmem_fence_before();
       mbar_arrive(&bar.ds_full);
     }
-    if (ok) ok = warp_wait(&bar.o_full, 0, &bar.abort);
-    if (ok) {
-      tmem_fence_after();
-      const bool fine = put_half_row<HD / 2>(t_dq + lanes, a.dq + (long long)i * a.dq_row + h * a.dq_head, half * (HD / 2), a.head_dim, a.scale, mine);
-      if (mine && !fine) bar.bad[r] = 1;
+    if (ok && tiles > 0) ok = warp_wait(&bar.o_full, 0, &bar.abort);
+    tmem_fence_after();
+    if (split == 1) {
+      if (ok) {
+        const bool fine = put_row<HD / 2>(t_dq + lanes, a.dq + (long long)i * a.dq_row + h * a.dq_head, half * (HD / 2), a.head_dim, a.scale, mine);
+        if (mine && !fine) bar.bad[r] = 1;
+      }
+    } else if (ok) {
+      // every operand has been read: the tiles' place takes this block's sums
+      if (tiles > 0) stage_row<HD / 2>(t_dq + lanes + half * (HD / 2), smem + half * (HD / 2) * kRows * 4, r);
+      else
+        for (int c = half * (HD / 8); c < (half + 1) * (HD / 8); ++c)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(smem + (c * kRows + r) * 16), "r"(0) : "memory");
     }
-    math_sync(); // both halves are written before a row is written again
-    if (ok && half == 0)
+    if (split == 1) {
+      math_sync(); // both halves are written before a row is written again
+    } else {
+      cluster_sync(); // all blocks' sums are staged
+      // eight columns at a time, dealt to the cluster's blocks and both halves
+      if (mine && !bar.abort)
+        for (int c = (part * 2 + half) * 8; c < a.head_dim; c += split * 16) {
+          float v[8];
+          sum_staged(v, smem, split, c, r);
+          if (!put8(a.dq + (long long)i * a.dq_row + h * a.dq_head + c, v, a.scale)) mark_remote(smem_u32(&bar.bad[r]));
+        }
+      cluster_sync(); // and read: the row is written, and marked in the first block where it is not finite
+    }
+    if (half == 0 && part == 0 && !bar.abort)
       for (unsigned again = __ballot_sync(0xffffffffu, bar.bad[r] != 0); again; again &= again - 1)
         attn_dq_row(a, i - lane + __ffs(again) - 1, h, at.first, lane);
   }
@@ -284,15 +281,16 @@ struct DkvBarriers {
 template <int HD>
 __global__ void __launch_bounds__(kBwdThreads, 1)
     attn_dkv_kernel(const AttnArgs a, const __grid_constant__ HeadMap mq, const __grid_constant__ HeadMap mk, const __grid_constant__ HeadMap mv,
-                    const __grid_constant__ HeadMap mdo, int slots) {
+                    const __grid_constant__ HeadMap mdo, int split) {
   using L = BwdLayout<HD>;
   extern __shared__ unsigned char raw_smem[];
   __shared__ DkvBarriers bar;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int g = blockIdx.x % a.kv_heads;
+  const int part = cluster_rank(), unit = blockIdx.x / split, g = unit % a.kv_heads;
   grid_wait(); // delta is the work of the kernel before this one
-  const Place at = place_of(a, (int)(blockIdx.x / a.kv_heads), kRows);
+  const Place at = place_of<true>(a, unit / a.kv_heads, kRows);
   if (at.block < 0) {
+    if (part != 0) return;
     const int r0 = at.first + (-1 - at.block) * kRows;
     for (int r = r0 + warp; r < min(r0 + kRows, at.end); r += kBwdThreads / 32)
       for (int c = lane; c < a.head_dim; c += 32) {
@@ -303,7 +301,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   }
   const int k0 = at.first + at.block * kRows; // first key
   if (k0 >= at.end) return;
-  const int per_head = (at.end - k0 + kRows - 1) / kRows, tiles = per_head * a.group; // query tiles
+  const int per_head = (at.end - k0 + kRows - 1) / kRows, all = per_head * a.group; // query tiles
+  const int tiles = (all - part + split - 1) / split;                              // this block's: part, part + split, ...
   const unsigned smem = (smem_u32(raw_smem) + 1023) & ~1023u;
   const unsigned s_k = smem + L::kOwn, s_v = s_k + L::kTileBytes, s_q = smem + L::kRing, s_do = s_q + kStages * L::kTileBytes;
   // minus log-sum-exp (times log2 e) and minus delta of a query tile's rows
@@ -326,14 +325,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   const unsigned tmem = bar.tmem, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = t_dv + HD;
 
   if (warp >= 8) {
-    registers_down<kOtherRegs>();
     if (warp == 9 && lane == 0) {
       int issued = 0;
-      mbar_expect_tx(&bar.own_full, 2 * L::kTileBytes);
-      load_tile<HD>(s_k, mk, g, k0, &bar.own_full);
-      load_tile<HD>(s_v, mv, g, k0, &bar.own_full);
+      if (tiles > 0) {
+        mbar_expect_tx(&bar.own_full, 2 * L::kTileBytes);
+        load_tile<HD>(s_k, mk, g, k0, &bar.own_full);
+        load_tile<HD>(s_v, mv, g, k0, &bar.own_full);
+      }
       for (int it = 0; it < tiles; ++it) {
-        const int s = it % kStages, h = g * a.group + it / per_head, row = k0 + (it % per_head) * kRows;
+        const int s = it % kStages, n = it * split + part, h = g * a.group + n / per_head, row = k0 + (n % per_head) * kRows;
         if (!wait_or_abort(&bar.empty[s], ((it / kStages) & 1) ^ 1, &bar.abort)) break;
         mbar_expect_tx(&bar.q_full[s], L::kTileBytes);
         load_tile<HD>(s_q + s * L::kTileBytes, mq, h, row, &bar.q_full[s]);
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       if (issued < 2 * tiles) land_copies<kStages>(issued, &bar.own_full, bar.q_full, bar.do_full);
     } else if (warp == 10) {
       for (int it = 0; it < tiles; ++it) {
-        const int s = it % kStages, h = g * a.group + it / per_head, row = k0 + (it % per_head) * kRows;
+        const int s = it % kStages, n = it * split + part, h = g * a.group + n / per_head, row = k0 + (n % per_head) * kRows;
         if (!warp_wait(&bar.stat_empty[s], ((it / kStages) & 1) ^ 1, &bar.abort)) break;
         float *to = stats + s * 2 * kRows;
 #pragma unroll
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         }
         mbar_arrive(&bar.stat_full[s]);
       }
-    } else if (warp == 8 && lane == 0) {
+    } else if (warp == 8 && lane == 0 && tiles > 0) {
       constexpr unsigned kk = mma_desc(128, false, false), kn = mma_desc(HD, false, true);
       bool ok = wait_or_abort(&bar.own_full, 0, &bar.abort) && wait_or_abort(&bar.q_full[0], 0, &bar.abort);
       if (ok) {
@@ -398,8 +398,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         }
       }
     }
+    __syncwarp();
+    if (split > 1) {
+      cluster_sync();
+      cluster_sync();
+    }
   } else {
-    registers_up<kMathRegs>();
     const int half = warp >> 2, r = threadIdx.x & 127, j0 = k0 + r; // this thread's key, and its half of the queries
     const bool mine = j0 < at.end;
     const unsigned lanes = (unsigned)(warp & 3) << 21;
@@ -407,7 +411,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     const float c = a.scale_log2;
     bool ok = true;
     for (int it = 0; it < tiles; ++it) {
-      const int st = it % kStages, t = it % per_head;
+      const int st = it % kStages, t = (it * split + part) % per_head;
       const unsigned ph = (it / kStages) & 1;
       const int valid = at.end - (k0 + t * kRows); // query rows of this tile inside the sequence
       const bool edge = t == 0 || valid < kRows;
@@ -430,7 +434,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       auto weights = [&](auto masked) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          unsigned x[16];
+          unsigned x[8];
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
             const float4 m = lse[u * 8 + j / 4];
@@ -442,9 +446,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
               if (decltype(masked)::value && hidden(u, j + e)) p[e] = 0.f;
               s[u][j + e] = __float_as_uint(p[e]);
             }
-            x[j / 2] = bf16_pair(p[0], p[1]), x[j / 2 + 1] = bf16_pair(p[2], p[3]);
+            x[j / 2 % 8] = bf16_pair(p[0], p[1]), x[j / 2 % 8 + 1] = bf16_pair(p[2], p[3]);
+            if (j % 16 == 12) tmem_store8(t_s + half * 64 + u * 16 + j / 16 * 8 + lanes, x);
           }
-          tmem_store16(t_s + half * 64 + u * 16 + lanes, x);
         }
       };
       if (edge) weights(std::true_type{});
@@ -468,7 +472,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       auto slopes = [&](auto masked) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          unsigned d[32], x[16];
+          unsigned d[32], x[8];
           tmem_load32(t_dp + half * 64 + u * 32 + lanes, d);
           tmem_wait_load();
 #pragma unroll
@@ -484,9 +488,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
               if (hidden(u, j + 2)) y[1].x = 0.f;
               if (hidden(u, j + 3)) y[1].y = 0.f;
             }
-            x[j / 2] = bf16_pair(y[0].x, y[0].y), x[j / 2 + 1] = bf16_pair(y[1].x, y[1].y);
+            x[j / 2 % 8] = bf16_pair(y[0].x, y[0].y), x[j / 2 % 8 + 1] = bf16_pair(y[1].x, y[1].y);
+            if (j % 16 == 12) tmem_store8(t_dp + half * 64 + u * 16 + j / 16 * 8 + lanes, x);
           }
-          tmem_store16(t_dp + half * 64 + u * 16 + lanes, x);
         }
       };
       if (edge) slopes(std::true_type{});
@@ -496,15 +500,35 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       mbar_arrive(&bar.ds_full);
       mbar_arrive(&bar.stat_empty[st]);
     }
-    if (ok) ok = warp_wait(&bar.o_full, 0, &bar.abort);
-    if (ok) {
-      tmem_fence_after();
-      bool fine = put_half_row<HD / 2>(t_dv + lanes, a.dv + (long long)j0 * a.dv_row + g * a.dv_head, half * (HD / 2), a.head_dim, 1.f, mine);
-      fine &= put_half_row<HD / 2>(t_dk + lanes, a.dk + (long long)j0 * a.dk_row + g * a.dk_head, half * (HD / 2), a.head_dim, a.scale, mine);
-      if (mine && !fine) bar.bad[r] = 1;
+    if (ok && tiles > 0) ok = warp_wait(&bar.o_full, 0, &bar.abort);
+    tmem_fence_after();
+    if (split == 1) {
+      if (ok) {
+        bool fine = put_row<HD / 2>(t_dv + lanes, a.dv + (long long)j0 * a.dv_row + g * a.dv_head, half * (HD / 2), a.head_dim, 1.f, mine);
+        fine &= put_row<HD / 2>(t_dk + lanes, a.dk + (long long)j0 * a.dk_row + g * a.dk_head, half * (HD / 2), a.head_dim, a.scale, mine);
+        if (mine && !fine) bar.bad[r] = 1;
+      }
+    } else if (ok) {
+      // every operand has been read: the tiles' place takes this block's sums, dv by warps 0-3, dk by warps 4-7
+      const unsigned to = smem + half * HD * kRows * 4;
+      if (tiles > 0) stage_row<HD>((half ? t_dk : t_dv) + lanes, to, r);
+      else
+        for (int c = 0; c < HD / 4; ++c) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + (c * kRows + r) * 16), "r"(0) : "memory");
     }
-    math_sync();
-    if (ok && half == 0)
+    if (split == 1) {
+      math_sync(); // both halves are written before a row is written again
+    } else {
+      cluster_sync(); // all blocks' sums are staged
+      __nv_bfloat16 *row = half ? a.dk + (long long)j0 * a.dk_row + g * a.dk_head : a.dv + (long long)j0 * a.dv_row + g * a.dv_head;
+      if (mine && !bar.abort)
+        for (int c = part * 8; c < a.head_dim; c += split * 8) {
+          float v[8];
+          sum_staged(v, smem + half * HD * kRows * 4, split, c, r);
+          if (!put8(row + c, v, half ? a.scale : 1.f)) mark_remote(smem_u32(&bar.bad[r]));
+        }
+      cluster_sync(); // and read: the row is written, and marked in the first block where it is not finite
+    }
+    if (half == 0 && part == 0 && !bar.abort)
       for (unsigned again = __ballot_sync(0xffffffffu, bar.bad[r] != 0); again; again &= again - 1)
         attn_dkv_row(a, j0 - lane + __ffs(again) - 1, g, at.end, lane);
   }
@@ -521,12 +545,14 @@ template <int HD> int launch(const AttnArgs &a, const HeadMap &mq, const HeadMap
   constexpr int bytes = BwdLayout<HD>::kBytes;
   static OncePerDevice once;
   if (!once.get([] { return allow_smem(attn_dq_kernel<HD>, bytes) && allow_smem(attn_dkv_kernel<HD>, bytes); })) return DILOCO_ERR_CUDA;
-  const long long slots = (long long)a.tokens / kRows + a.sequences + 1;
-  if (slots * a.heads > INT32_MAX) return DILOCO_ERR_UNSUPPORTED;
-  attn_dq_kernel<HD><<<(unsigned)(slots * a.heads), kBwdThreads, bytes, s>>>(a, mq, mk, mv, mdo, (int)slots);
-  const int rc = launched();
+  int dev = 0;
+  cudaGetDevice(&dev);
+  const int sms = sm_count(dev);
+  const long long ranks = ranks_of(a, kRows);
+  const int by_q = split_of(a, kRows, a.heads, 1, sms), by_k = split_of(a, kRows, a.kv_heads, a.group, sms);
+  const int rc = launch_split(attn_dq_kernel<HD>, ranks * a.heads, by_q, kBwdThreads, bytes, s, false, a, mq, mk, mv, mdo, by_q);
   if (rc != DILOCO_OK) return rc;
-  return launch_chained(attn_dkv_kernel<HD>, dim3((unsigned)(slots * a.kv_heads)), dim3(kBwdThreads), bytes, s, a, mq, mk, mv, mdo, (int)slots);
+  return launch_split(attn_dkv_kernel<HD>, ranks * a.kv_heads, by_k, kBwdThreads, bytes, s, true, a, mq, mk, mv, mdo, by_k);
 }
 
 } // namespace

@@ -10,7 +10,9 @@ namespace diloco {
 
 constexpr unsigned long long kOpWaitNs = 1000000000ull; // bound of one wait
 
-// A wait that gives up raises `abort` (shared memory) so that every role of the block leaves its loop.
+// A wait that gives up raises `abort` (shared memory) so that every role of the block leaves its loop.  Each poll after
+// the first looks at the clock, which also spaces them: polls without it, or with a suspension time, took issue slots from
+// the arithmetic beside them (1 to 3 % of the kernels).
 __device__ __forceinline__ bool wait_or_abort(unsigned long long *bar, unsigned parity, volatile unsigned *abort) {
   if (mbar_try_wait(bar, parity)) return true;
   if (mbar_wait_bounded(bar, parity, kOpWaitNs, abort)) return true;
@@ -69,6 +71,10 @@ __device__ __forceinline__ void tmem_store16(unsigned at, const unsigned (&v)[16
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::DILOCO_I8(v, 0),
                DILOCO_I8(v, 8), "r"(at)
                : "memory");
+}
+
+__device__ __forceinline__ void tmem_store8(unsigned at, const unsigned (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::DILOCO_I8(v, 0), "r"(at) : "memory");
 }
 
 // ------------------------------------------------------------------------- matrix instructions
