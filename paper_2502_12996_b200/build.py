@@ -1,4 +1,5 @@
-"""In-tree build of libdiloco.so with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""In-tree build of libdiloco.so with nvcc for sm_100a (cross-compiles without a GPU), and of the
+extension module that calls its operators on torch tensors."""
 from __future__ import annotations
 
 import os
@@ -27,11 +28,40 @@ STEP_FLAGS = ["-fmad=false"]             # the steps: no FMA contraction, one ro
 
 
 def _stale() -> bool:
-    if not LIB.exists():
+    if not LIB.exists() or not _torch_extension().exists():
         return True
     t = LIB.stat().st_mtime
-    deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + [PKG.parent / "include" / "diloco.h", Path(__file__)]
+    deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(CSRC.glob("*.cpp")) + [PKG.parent / "include" / "diloco.h", Path(__file__)]
     return any(d.stat().st_mtime > t for d in deps)
+
+
+def _torch_extension() -> Path:
+    """Where the extension module over torch tensors is built (beside the library that it is linked against)."""
+    import sysconfig
+    return PKG / ("_diloco_ops" + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
+def _build_torch_extension() -> str:
+    """Compile and link csrc/diloco_torch.cpp with the host compiler against torch and libdiloco.so ($ORIGIN)."""
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension
+    out = _torch_extension()
+    tmp = OBJ / (out.name + f".tmp{os.getpid()}")
+    cuda = Path(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")).resolve().parent.parent
+    # the system's compiler, whatever CXX says: one that links libstdc++ statically gives the module a second copy beside
+    # torch's, and formatting an error message across the two crashes
+    cmd = ["g++", "-shared-libgcc", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-DTORCH_EXTENSION_NAME=_diloco_ops",
+           "-DTORCH_API_INCLUDE_EXTENSION_H", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd += [f"-isystem{p}" for p in cpp_extension.include_paths()] + [f"-isystem{cuda}/include", f"-isystem{sysconfig.get_paths()['include']}"]
+    cmd += [str(CSRC / "diloco_torch.cpp"), "-o", str(tmp)] + [f"-L{p}" for p in cpp_extension.library_paths()] + [f"-L{PKG}"]
+    cmd += ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch", "-ltorch_python", "-l:libdiloco.so", "-Wl,-rpath,$ORIGIN"]
+    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if res.returncode != 0:
+        print(res.stdout)
+        raise subprocess.CalledProcessError(res.returncode, cmd)
+    os.replace(tmp, out)
+    return res.stdout
 
 
 def _compile(nvcc: str, src: Path, obj: Path, flags) -> str:
@@ -62,8 +92,10 @@ def build_library(force: bool = False, verbose: bool = False) -> Path:
     report = "\n".join(logs)
     if verbose:
         print(report)
-    REPORT.write_text(report)
     os.replace(tmp, LIB)
+    _build_torch_extension()
+    REPORT.write_text(report)
+    os.utime(LIB)
     return LIB
 
 

@@ -1,0 +1,294 @@
+// Decoder operators of include/diloco.h on torch tensors: what the ops module calls.  Checks shapes, types, strides and
+// devices, allocates outputs and workspaces from torch's allocator on the current stream, and calls the C ABI.  A call
+// through ctypes took 11 to 15 us on the host, longer than the smallest kernels; this one takes 4 to 6.
+#include <ATen/cuda/CUDAContext.h>
+#include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
+#include <torch/extension.h>
+
+#include "../../include/diloco.h"
+
+namespace py = pybind11;
+using at::Tensor;
+using OptTensor = std::optional<Tensor>;
+
+namespace {
+
+[[noreturn]] void raise_status(int64_t status, const char *where) {
+  const py::object cls = py::module_::import("paper_2502_12996_b200.binding").attr("DilocoError");
+  const py::object e = cls(status, where);
+  PyErr_SetObject(cls.ptr(), e.ptr());
+  throw py::error_already_set();
+}
+void check(int status, const char *where) {
+  if (status != DILOCO_OK) raise_status(status, where);
+}
+
+int32_t dtype_of(at::ScalarType t, const char *name) {
+  if (t == at::kFloat) return DILOCO_DTYPE_F32;
+  TORCH_CHECK_TYPE(t == at::kBFloat16, name, ": float32 or bfloat16 wanted, got ", t);
+  return DILOCO_DTYPE_BF16;
+}
+int32_t ids_kind(const Tensor &t, const char *name) {
+  if (t.scalar_type() == at::kInt) return 0;
+  TORCH_CHECK_TYPE(t.scalar_type() == at::kLong, name, ": int32 or int64 wanted, got ", t.scalar_type());
+  return 1;
+}
+
+// The one CUDA device of a call's tensors.
+struct Device {
+  c10::Device device;
+  explicit Device(const Tensor &first) : device(first.device()) {
+    TORCH_CHECK_VALUE(first.is_cuda(), "CUDA tensors are wanted, got one on ", first.device());
+  }
+  Device &also(const Tensor &t) {
+    TORCH_CHECK_VALUE(t.device() == device, "all tensors of a call have to be on one CUDA device: ", t.device(), " and ", device);
+    return *this;
+  }
+  Device &also(const OptTensor &t) { return t ? also(*t) : *this; }
+  void *stream() const { return at::cuda::getCurrentCUDAStream(device.index()).stream(); }
+  Tensor empty(at::IntArrayRef shape, at::ScalarType t) const { return at::detail::empty_cuda(shape, t, device, std::nullopt); }
+  Tensor bytes(int64_t n, const char *where) const {
+    if (n < 0) raise_status(n, where);
+    return empty({n > 0 ? n : 1}, at::kByte);
+  }
+};
+
+void *ptr(const Tensor &t) { return t.data_ptr(); }
+void *ptr(const OptTensor &t) { return t ? t->data_ptr() : nullptr; }
+
+// Every axis but the first contiguous; axes of one element may carry any stride.
+bool rest_contiguous(const Tensor &t, int64_t from) {
+  int64_t n = 1;
+  for (int64_t i = t.dim() - 1; i >= from; --i) {
+    if (t.size(i) != 1 && t.stride(i) != n) return t.numel() == 0;
+    n *= t.size(i);
+  }
+  return true;
+}
+bool contiguous_f32(const Tensor &t, at::IntArrayRef shape) { return t.scalar_type() == at::kFloat && t.sizes() == shape && rest_contiguous(t, 0); }
+
+// A parameter or its gradient, [M, ...] with each replica's part contiguous: the distance between replicas.
+int64_t replica_stride(const Tensor &t, at::IntArrayRef shape, const char *name) {
+  TORCH_CHECK_VALUE(t.sizes() == shape, name, ": shape ", shape, " wanted, got ", t.sizes());
+  TORCH_CHECK_VALUE(rest_contiguous(t, 1), name, ": each replica's part has to be contiguous");
+  return shape[0] > 1 ? t.stride(0) : t.numel();
+}
+
+// -------------------------------------------------------------------------------- embedding
+diloco_embedding_t embedding_desc(const Tensor &ids, const Tensor &table, const Tensor &rows, double scale, const char *what) {
+  TORCH_CHECK_VALUE(ids.dim() == 2, "ids: [M, tokens] wanted, got shape ", ids.sizes());
+  TORCH_CHECK_VALUE(table.dim() == 3 && table.size(0) == ids.size(0), what, ": [M, vocab, d] with M = ", ids.size(0), " wanted, got ", table.sizes());
+  const int64_t M = ids.size(0), tokens = ids.size(1), V = table.size(1), d = table.size(2);
+  diloco_embedding_t e = {};
+  e.ids_int64 = ids_kind(ids, "ids");
+  e.M = (int32_t)M, e.d = (int32_t)d, e.tokens = tokens, e.vocab = V, e.scale = (float)scale;
+  e.table_stride = e.grad_stride = replica_stride(table, {M, V, d}, what);
+  TORCH_CHECK_VALUE(rows.sizes() == at::IntArrayRef({M, tokens, d}), "rows: shape [", M, ", ", tokens, ", ", d, "] wanted, got ", rows.sizes());
+  const int64_t row = tokens > 1 ? rows.stride(1) : M > 1 ? rows.stride(0) : d;
+  TORCH_CHECK_VALUE(d == 1 || rows.stride(2) == 1, "rows: the last axis has to be contiguous");
+  TORCH_CHECK_VALUE(M == 1 || tokens == 0 || rows.stride(0) == tokens * row, "rows: replicas have to follow one another at the tokens' stride");
+  e.row_stride = row > d ? row : d;
+  e.table_dtype = e.grad_dtype = dtype_of(table.scalar_type(), what);
+  e.act_dtype = dtype_of(rows.scalar_type(), "rows");
+  return e;
+}
+
+Tensor embedding_forward(const Tensor &ids_in, const Tensor &table, double scale, std::optional<at::ScalarType> out_dtype, const OptTensor &out_in) {
+  Device dev(table);
+  dev.also(ids_in).also(out_in);
+  const c10::cuda::CUDAGuard guard(dev.device);
+  const Tensor ids = ids_in.is_contiguous() ? ids_in : ids_in.contiguous();
+  TORCH_CHECK_VALUE(ids.dim() == 2 && table.dim() == 3, "ids: [M, tokens], table: [M, vocab, d] wanted");
+  const at::ScalarType t = out_dtype.value_or(table.scalar_type());
+  dtype_of(t, "out");
+  const Tensor out = out_in ? *out_in : dev.empty({ids.size(0), ids.size(1), table.size(2)}, t);
+  const diloco_embedding_t e = embedding_desc(ids, table, out, scale, "table");
+  check(diloco_embedding_forward(&e, ptr(ids), ptr(table), ptr(out), dev.stream()), "diloco_embedding_forward");
+  return out;
+}
+
+Tensor embedding_backward(const Tensor &ids_in, const Tensor &dout, const Tensor &dtable, double scale, bool accumulate) {
+  Device dev(dtable);
+  dev.also(ids_in).also(dout);
+  const c10::cuda::CUDAGuard guard(dev.device);
+  const Tensor ids = ids_in.is_contiguous() ? ids_in : ids_in.contiguous();
+  const diloco_embedding_t e = embedding_desc(ids, dtable, dout, scale, "dtable");
+  const int64_t n = diloco_embedding_workspace_bytes(&e);
+  const Tensor ws = dev.bytes(n, "diloco_embedding_workspace_bytes");
+  check(diloco_embedding_backward(&e, ptr(ids), ptr(dout), ptr(dtable), accumulate, ptr(ws), n, dev.stream()), "diloco_embedding_backward");
+  return dtable;
+}
+
+// ------------------------------------------------------------------------------- layer norm
+// [M, rows, groups, d] (or [M, rows, d]) with one row stride over all replicas.
+void norm_rows(const Tensor &t, const Tensor &x, const char *name, int64_t &row, int64_t &group) {
+  TORCH_CHECK_VALUE(t.sizes() == x.sizes(), name, ": shape ", x.sizes(), " wanted, got ", t.sizes());
+  TORCH_CHECK_VALUE(t.scalar_type() == x.scalar_type(), name, ": the type of x wanted");
+  const int64_t M = t.size(0), N = t.size(1);
+  TORCH_CHECK_VALUE(t.size(-1) == 1 || t.stride(-1) == 1, name, ": the last axis has to be contiguous");
+  row = N > 1 ? t.stride(1) : M > 1 ? t.stride(0) : 0;
+  TORCH_CHECK_VALUE(M == 1 || N <= 1 || t.stride(0) == N * row, name, ": replicas have to follow one another at the rows' stride");
+  group = t.dim() == 4 && t.size(2) > 1 ? t.stride(2) : 0;
+}
+diloco_layernorm_t norm_desc(const Tensor &x, const Tensor &weight, double eps) {
+  TORCH_CHECK_VALUE(x.dim() == 3 || x.dim() == 4, "x: [M, rows, d] or [M, rows, groups, d] wanted, got shape ", x.sizes());
+  diloco_layernorm_t n = {};
+  n.M = (int32_t)x.size(0), n.d = (int32_t)x.size(-1), n.groups = x.dim() == 4 ? (int32_t)x.size(2) : 1, n.rows = x.size(1), n.eps = (float)eps;
+  n.act_dtype = dtype_of(x.scalar_type(), "x"), n.param_dtype = dtype_of(weight.scalar_type(), "weight");
+  norm_rows(x, x, "x", n.x_row_stride, n.x_group_stride);
+  n.param_stride = replica_stride(weight, {x.size(0), x.size(-1)}, "weight");
+  return n;
+}
+
+std::tuple<Tensor, Tensor, Tensor> layer_norm_forward(const Tensor &x, const Tensor &weight, const OptTensor &bias, double eps, const OptTensor &out_in) {
+  Device dev(x);
+  dev.also(weight).also(bias).also(out_in);
+  const c10::cuda::CUDAGuard guard(dev.device);
+  diloco_layernorm_t n = norm_desc(x, weight, eps);
+  if (bias) {
+    TORCH_CHECK_VALUE(bias->scalar_type() == weight.scalar_type(), "bias: the weight's type wanted");
+    TORCH_CHECK_VALUE(replica_stride(*bias, weight.sizes(), "bias") == n.param_stride, "bias: the weight's stride between replicas wanted");
+  }
+  const Tensor out = out_in ? *out_in : dev.empty(x.sizes(), x.scalar_type());
+  norm_rows(out, x, "out", n.y_row_stride, n.y_group_stride);
+  const at::IntArrayRef stat = x.sizes().slice(0, x.dim() - 1);
+  const Tensor mean = dev.empty(stat, at::kFloat), rstd = dev.empty(stat, at::kFloat);
+  check(diloco_layernorm_forward(&n, ptr(x), ptr(weight), ptr(bias), ptr(out), (float *)ptr(mean), (float *)ptr(rstd), dev.stream()),
+        "diloco_layernorm_forward");
+  return {out, mean, rstd};
+}
+
+Tensor layer_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &weight, const Tensor &mean, const Tensor &rstd, const OptTensor &dweight,
+                           const OptTensor &dbias, bool accumulate, const OptTensor &dx_in) {
+  Device dev(x);
+  dev.also(dy).also(weight).also(mean).also(rstd).also(dweight).also(dbias).also(dx_in);
+  const c10::cuda::CUDAGuard guard(dev.device);
+  diloco_layernorm_t n = norm_desc(x, weight, 0.0);
+  norm_rows(dy, x, "dy", n.y_row_stride, n.y_group_stride);
+  const at::IntArrayRef stat = x.sizes().slice(0, x.dim() - 1);
+  TORCH_CHECK_VALUE(contiguous_f32(mean, stat) && contiguous_f32(rstd, stat), "mean, rstd: contiguous float32 ", stat, " wanted");
+  const Tensor *grad = dweight ? &*dweight : dbias ? &*dbias : nullptr;
+  Tensor ws;
+  int64_t bytes = 0;
+  if (grad) {
+    n.grad_dtype = dtype_of(grad->scalar_type(), "dweight");
+    n.grad_stride = replica_stride(*grad, weight.sizes(), "dweight");
+    if (dweight && dbias)
+      TORCH_CHECK_VALUE(dbias->scalar_type() == grad->scalar_type() && replica_stride(*dbias, weight.sizes(), "dbias") == n.grad_stride,
+                        "dbias: the type and stride of dweight wanted");
+    bytes = diloco_layernorm_workspace_bytes(&n);
+    ws = dev.bytes(bytes, "diloco_layernorm_workspace_bytes");
+  }
+  const Tensor dx = dx_in ? *dx_in : dev.empty(x.sizes(), x.scalar_type());
+  norm_rows(dx, x, "dx", n.dx_row_stride, n.dx_group_stride);
+  check(diloco_layernorm_backward(&n, ptr(dy), ptr(x), ptr(weight), (const float *)ptr(mean), (const float *)ptr(rstd), ptr(dx), ptr(dweight), ptr(dbias),
+                                  accumulate, grad ? ptr(ws) : nullptr, bytes, dev.stream()),
+        "diloco_layernorm_backward");
+  return dx;
+}
+
+// -------------------------------------------------------------------------------- attention
+void heads_of(const Tensor &t, const char *name, int64_t tokens, int64_t heads, int64_t d, int64_t &row, int64_t &head) {
+  TORCH_CHECK_TYPE(t.scalar_type() == at::kBFloat16, name, ": bfloat16 wanted, got ", t.scalar_type());
+  TORCH_CHECK_VALUE(t.sizes() == at::IntArrayRef({tokens, heads, d}), name, ": shape [", tokens, ", ", heads, ", ", d, "] wanted, got ", t.sizes());
+  TORCH_CHECK_VALUE(d == 1 || t.stride(2) == 1, name, ": the last axis has to be contiguous");
+  // an axis of one element may carry any stride; a contiguous one is passed in its place
+  row = tokens > 1 ? t.stride(0) : heads * d;
+  head = heads > 1 ? t.stride(1) : d;
+}
+diloco_attention_t attention_desc(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &cu, std::optional<double> scale, int64_t status) {
+  TORCH_CHECK_VALUE(q.dim() == 3 && k.dim() == 3, "q, k, v: [tokens, heads, head_dim] wanted");
+  TORCH_CHECK_TYPE(cu.scalar_type() == at::kInt, "cu_seqlens: int32 wanted, got ", cu.scalar_type());
+  TORCH_CHECK_VALUE(cu.dim() == 1 && cu.numel() >= 1 && rest_contiguous(cu, 0), "cu_seqlens: a contiguous vector of sequences + 1 wanted");
+  diloco_attention_t a = {};
+  const int64_t T = q.size(0), H = q.size(1), K = k.size(1), D = q.size(2);
+  a.heads = (int32_t)H, a.kv_heads = (int32_t)K, a.head_dim = (int32_t)D, a.sequences = (int32_t)(cu.numel() - 1), a.tokens = T;
+  a.scale = scale ? (float)*scale : 1.f / std::sqrt((float)D);
+  a.device_status = reinterpret_cast<uint32_t *>(status);
+  heads_of(q, "q", T, H, D, a.q_row_stride, a.q_head_stride);
+  heads_of(k, "k", T, K, D, a.k_row_stride, a.k_head_stride);
+  heads_of(v, "v", T, K, D, a.v_row_stride, a.v_head_stride);
+  return a;
+}
+
+std::tuple<Tensor, Tensor> attention_forward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &cu, std::optional<double> scale,
+                                             const OptTensor &out_in, int64_t status) {
+  Device dev(q);
+  dev.also(k).also(v).also(cu).also(out_in);
+  const c10::cuda::CUDAGuard guard(dev.device);
+  diloco_attention_t a = attention_desc(q, k, v, cu, scale, status);
+  const Tensor out = out_in ? *out_in : dev.empty(q.sizes(), q.scalar_type());
+  heads_of(out, "out", a.tokens, a.heads, a.head_dim, a.o_row_stride, a.o_head_stride);
+  const Tensor lse = dev.empty({a.heads, a.tokens}, at::kFloat);
+  check(diloco_attention_forward(&a, ptr(q), ptr(k), ptr(v), (const int32_t *)ptr(cu), ptr(out), (float *)ptr(lse), dev.stream()),
+        "diloco_attention_forward");
+  return {out, lse};
+}
+
+std::tuple<Tensor, Tensor, Tensor> attention_backward(const Tensor &dout, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &out,
+                                                      const Tensor &lse, const Tensor &cu, std::optional<double> scale, const OptTensor &dq_in,
+                                                      const OptTensor &dk_in, const OptTensor &dv_in, int64_t status) {
+  Device dev(q);
+  dev.also(k).also(v).also(cu).also(out).also(lse).also(dout).also(dq_in).also(dk_in).also(dv_in);
+  const c10::cuda::CUDAGuard guard(dev.device);
+  diloco_attention_t a = attention_desc(q, k, v, cu, scale, status);
+  const int64_t T = a.tokens, H = a.heads, K = a.kv_heads, D = a.head_dim;
+  TORCH_CHECK_VALUE(contiguous_f32(lse, {H, T}), "lse: contiguous float32 [", H, ", ", T, "] wanted");
+  heads_of(out, "out", T, H, D, a.o_row_stride, a.o_head_stride);
+  heads_of(dout, "dout", T, H, D, a.do_row_stride, a.do_head_stride);
+  const Tensor dq = dq_in ? *dq_in : dev.empty(q.sizes(), q.scalar_type()), dk = dk_in ? *dk_in : dev.empty(k.sizes(), k.scalar_type()),
+               dv = dv_in ? *dv_in : dev.empty(v.sizes(), v.scalar_type());
+  heads_of(dq, "dq", T, H, D, a.dq_row_stride, a.dq_head_stride);
+  heads_of(dk, "dk", T, K, D, a.dk_row_stride, a.dk_head_stride);
+  heads_of(dv, "dv", T, K, D, a.dv_row_stride, a.dv_head_stride);
+  const int64_t n = diloco_attention_workspace_bytes(&a);
+  const Tensor ws = dev.bytes(n, "diloco_attention_workspace_bytes");
+  check(diloco_attention_backward(&a, ptr(dout), ptr(q), ptr(k), ptr(v), ptr(out), (const float *)ptr(lse), (const int32_t *)ptr(cu), ptr(dq), ptr(dk),
+                                  ptr(dv), ptr(ws), n, dev.stream()),
+        "diloco_attention_backward");
+  return {dq, dk, dv};
+}
+
+// ------------------------------------------------------------------------------------- loss
+std::tuple<Tensor, Tensor, OptTensor> distill_loss(const Tensor &logits, const Tensor &ids_in, const Tensor &teacher_in, double temperature, double z_coef,
+                                                   const OptTensor &row_weight, double grad_scale, bool grad, const OptTensor &dlogits_in) {
+  Device dev(logits);
+  dev.also(ids_in).also(teacher_in).also(row_weight).also(dlogits_in);
+  const c10::cuda::CUDAGuard guard(dev.device);
+  TORCH_CHECK_VALUE(logits.dim() == 2 && ids_in.dim() == 2, "logits: [rows, vocab], teacher_ids: [rows, k] wanted");
+  const int64_t N = logits.size(0), V = logits.size(1);
+  diloco_distill_t l = {};
+  l.ids_int64 = ids_kind(ids_in, "teacher_ids");
+  TORCH_CHECK_VALUE(ids_in.size(0) == N && teacher_in.sizes() == ids_in.sizes(), "teacher entries: shape (", N, ", k) wanted for both");
+  TORCH_CHECK_VALUE(V <= 1 || logits.stride(1) == 1, "logits: the last axis has to be contiguous");
+  TORCH_CHECK_VALUE(!row_weight || contiguous_f32(*row_weight, {N}), "row_weight: contiguous float32 (", N, ",) wanted");
+  const Tensor ids = ids_in.is_contiguous() ? ids_in : ids_in.contiguous(), teacher = teacher_in.is_contiguous() ? teacher_in : teacher_in.contiguous();
+  l.rows = N, l.vocab = V, l.k = (int32_t)ids.size(1), l.logits_stride = N > 1 ? logits.stride(0) : V;
+  l.dtype = dtype_of(logits.scalar_type(), "logits"), l.teacher_dtype = dtype_of(teacher.scalar_type(), "teacher_logits");
+  l.temperature = (float)temperature, l.z_coef = (float)z_coef, l.grad_scale = (float)grad_scale;
+  OptTensor dlogits = dlogits_in;
+  if (grad && !dlogits) dlogits = dev.empty(logits.sizes(), logits.scalar_type());
+  if (dlogits) {
+    TORCH_CHECK_VALUE(dlogits->sizes() == logits.sizes() && dlogits->scalar_type() == logits.scalar_type() && (V <= 1 || dlogits->stride(1) == 1),
+                      "dlogits: shape and type of logits wanted, the last axis contiguous");
+    l.grad_stride = N > 1 ? dlogits->stride(0) : V;
+  }
+  const Tensor loss = dev.empty({N}, at::kFloat), lse = dev.empty({N}, at::kFloat);
+  check(diloco_distill_loss(&l, ptr(logits), ptr(ids), ptr(teacher), (const float *)ptr(row_weight), (float *)ptr(loss), (float *)ptr(lse), ptr(dlogits),
+                            dev.stream()),
+        "diloco_distill_loss");
+  return {loss, lse, dlogits};
+}
+
+} // namespace
+
+PYBIND11_MODULE(_diloco_ops, m) {
+  m.def("embedding_forward", &embedding_forward);
+  m.def("embedding_backward", &embedding_backward);
+  m.def("layer_norm_forward", &layer_norm_forward);
+  m.def("layer_norm_backward", &layer_norm_backward);
+  m.def("attention_forward", &attention_forward);
+  m.def("attention_backward", &attention_backward);
+  m.def("distill_loss", &distill_loss);
+}
