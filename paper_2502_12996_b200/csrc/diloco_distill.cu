@@ -6,13 +6,17 @@
 //   dx_v = exp(x_v / T - lse) w (T + 2 z lse / T) - w T sum_{k: id_k = v} p_k
 //
 // A row of logits is read once and its gradient written once; memory bounds it as long as a row is not read
-// twice, so one block holds a whole row in registers (16-byte accesses, RV of them a thread): maximum, sum of
-// exponentials and gradient all come from that copy, while the next row is already on its way to shared memory.
+// twice from there.  Three forms, by the bytes of a row:
+//   staged    two rows fit an SM's shared memory (up to 110 KB): a block keeps one there; sum of exponentials and gradient
+//             read it from there, and each piece of the next row is on its way as soon as the gradient has read this
+//             one's.  Two or more blocks on an SM, so that one's exponentials (the special-function unit's 16 a cycle, twice an
+//             element, take 3/4 of the time that the row's bytes take) run beside another's loads and stores.
+//   resident  one row fits a block's registers (up to 138 KB): the row is in registers and the next one in shared memory
+//   stream    longer rows are read twice, the second time mostly from L2
 // One warp of the block has the teacher's entries and nothing else: their fetch, softmax and share of the loss, and the
-// elements of the gradient that they touch, are as long a chain of small steps as the row itself.  Rows that fit no
-// block are read twice, the second time mostly from L2.  Rows need not start on 16 bytes (an odd vocabulary): the
-// elements before the first and after the last whole access are taken one by one.  An element that several entries
-// point at is written once, with the sum of their shares, so nothing is added by atomics.
+// elements of the gradient that they touch, are as long a chain of small steps as the row itself.  Rows need not start on
+// 16 bytes (an odd vocabulary): the elements before the first and after the last whole access are taken one by one.  An
+// element that several entries point at is written once, with the sum of their shares, so nothing is added by atomics.
 #include <type_traits>
 
 #include "diloco_ops.cuh"
@@ -112,6 +116,7 @@ __device__ __forceinline__ RowScale row_scale(const DistillArgs &a, float m, flo
   r.coef = any ? wn * (a.temperature + 2.f * a.z * r.lse * a.inv_t) : 0.f;
   return r;
 }
+__device__ __forceinline__ float row_weight_of(const DistillArgs &a, long long n) { return a.grad_scale * (a.row_weight ? a.row_weight[n] : 1.f); }
 __device__ __forceinline__ float term(float x, float c, const RowScale &r) { return ex2(fmaf(x, c, -r.lse2)) * r.coef; }
 __device__ __forceinline__ void put_loss(const DistillArgs &a, long long n, const RowScale &r, float kl, float wn, bool any) {
   if ((threadIdx.x & 31) == 0) {
@@ -223,10 +228,124 @@ __device__ __forceinline__ uint4 terms(const uint4 &r, float2 c, float2 lse2, fl
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// Rows of at most (NT - 32) * RV accesses: NT - 32 threads for the row, the last warp for the teacher.  The next row is
-// on its way into shared memory (each thread copies what it will itself read, so no barrier is needed) while this
-// one is worked on.  The row's threads wait at one barrier a row, for the sums of all warps; the teacher's warp
-// reads the next row's entries behind it, waits for the row's gradient and writes its elements.
+// The teacher's warp of a block: reads the next row's entries behind the barrier for this row's sums, waits for the
+// row's gradient and writes its elements.  `row_bytes`: of the row's place in shared memory.
+template <typename T, int NT> __device__ __forceinline__ void teacher_warp(const DistillArgs &a, Partial *red, unsigned char *at) {
+  constexpr int NC = NT - 32;
+  auto row_of = [&](long long n) { return static_cast<const T *>(a.logits) + n * a.logits_stride; };
+  bool any = false;
+  float kl = 0.f;
+  long long n = blockIdx.x;
+  if (n < a.rows) kl = read_teacher<T>(a, Teacher(at, a.k), n, row_of(n), any);
+  for (int turn = 0; n < a.rows; n += gridDim.x, turn ^= 1) {
+    const Teacher t(at + turn * teacher_bytes(a.k), a.k);
+    const float wn = row_weight_of(a, n);
+    if (threadIdx.x == NC) red[turn].any = any;
+    block_sync<1, NT>();
+    float m, s;
+    get_partial(red[turn], NC / 32, m, s);
+    const RowScale r = row_scale(a, m, s, wn, any);
+    put_loss(a, n, r, kl, wn, any);
+    const bool put = a.dlogits && any;
+    if (n + gridDim.x < a.rows)
+      kl = read_teacher<T>(a, Teacher(at + (turn ^ 1) * teacher_bytes(a.k), a.k), n + gridDim.x, row_of(n + gridDim.x), any);
+    block_sync<2, NT>();
+    if (put) put_teacher<T>(a, t, static_cast<T *>(a.dlogits) + n * a.grad_stride, r);
+    __syncwarp();
+  }
+}
+
+// Staged form.  NT - 32 threads for the row, `slots` accesses each at most; every thread copies what it will itself read, so
+// one barrier a row is enough, the one for the sums of all warps.
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) distill_staged_kernel(const DistillArgs a, int slots) {
+  constexpr int W = 16 / (int)sizeof(T), NC = NT - 32;
+  using Raw = typename Pack<T, W>::raw;
+  extern __shared__ __align__(16) unsigned char staged[]; // [slots][NC] accesses, then two rows' teachers
+  __shared__ Partial red[2];                               // rows in turn
+  const int tid = threadIdx.x;
+  if (tid >= NC) {
+    teacher_warp<T, NT>(a, red, staged + slots * NC * 16);
+    return;
+  }
+  const float c = a.inv_t * kLog2e;
+  auto row_of = [&](long long n) { return static_cast<const T *>(a.logits) + n * a.logits_stride; };
+  long long n = blockIdx.x;
+  if (n >= a.rows) return;
+  const Raw *mine = reinterpret_cast<const Raw *>(staged) + tid;
+  const unsigned to = (unsigned)__cvta_generic_to_shared(staged) + tid * 16;
+  // the single elements before and after a row's whole accesses: one for each of the first head + tail threads
+  auto odd_of = [&](const Span &sp) { return tid < sp.head ? tid : tid < sp.head + sp.tail ? sp.body * W + tid : -1; };
+  Span sp = span_of<T, W>(row_of(n), a.vocab);
+  for (int v = tid, i = 0; v < sp.body; v += NC, ++i) copy_async16(to + i * NC * 16, row_of(n) + sp.head + (long long)v * W);
+  copy_commit();
+  int odd = odd_of(sp);
+  float single[1] = {-INFINITY};
+  if (odd >= 0) load_vec<T, 1>(row_of(n) + odd, single);
+  for (int turn = 0; n < a.rows; turn ^= 1) {
+    const long long next = n + gridDim.x;
+    const float wn = row_weight_of(a, n), one = single[0];
+    const int at = odd, head = sp.head, body = sp.body;
+    copy_wait();
+    // running maximum and sum, two accesses at a time
+    float m = one * c, m0 = m == -INFINITY ? 0.f : m; // nothing but -infinity (or no element): every term is 0
+    const float2 cc = make_float2(c, c);
+    float2 sum = make_float2(at >= 0 ? ex2(fmaf(one, c, -m0)) : 0.f, 0.f);
+#pragma unroll 2
+    for (int v = tid, i = 0; v < body; v += 2 * NC, i += 2) {
+      const bool both = v + NC < body;
+      const Raw x = mine[i * NC], y = mine[(both ? i + 1 : i) * NC];
+      const float top = fmaxf(pack_max(x), pack_max(y)) * c;
+      if (top > m) {
+        const float f = m == -INFINITY ? 1.f : ex2(m - top); // -infinity so far: the sum is 0 (or NaN)
+        sum = mul2(sum, make_float2(f, f));
+        m = m0 = top;
+      }
+      const float2 mm = make_float2(-m0, -m0);
+      add_terms(x, cc, mm, sum);
+      if (both) add_terms(y, cc, mm, sum);
+    }
+    put_partial(red[turn], m, sum.x + sum.y);
+    Span sn = sp;
+    single[0] = -INFINITY;
+    if (next < a.rows) {
+      sn = span_of<T, W>(row_of(next), a.vocab);
+      odd = odd_of(sn);
+      if (odd >= 0) load_vec<T, 1>(row_of(next) + odd, single);
+    }
+    block_sync<1, NT>();
+    const T *ahead = row_of(next) + sn.head;
+    if (a.dlogits) {
+      float s;
+      get_partial(red[turn], NC / 32, m, s);
+      const RowScale r = row_scale(a, m, s, wn, red[turn].any != 0);
+      T *grad = static_cast<T *>(a.dlogits) + n * a.grad_stride;
+      const float2 lse2 = make_float2(-r.lse2, -r.lse2), coef = make_float2(r.coef, r.coef);
+      Raw *out = reinterpret_cast<Raw *>(grad + head);
+#pragma unroll 4
+      for (int v = tid, i = 0; v < body; v += NC, ++i) {
+        const Raw x = mine[i * NC];
+        const Raw g = terms(x, cc, lse2, coef);
+        if (next < a.rows && v < sn.body) copy_async16(to + i * NC * 16, ahead + (long long)v * W); // x has been used
+        out[v] = g;
+      }
+      if (at >= 0) {
+        const float x[1] = {term(one, c, r)};
+        store_vec<T, 1>(grad + at, x);
+      }
+    }
+    if (next < a.rows) // what this row had no place for, or all of it
+      for (int i = a.dlogits ? (body - tid + NC - 1) / NC : 0, v = tid + i * NC; v < sn.body; v += NC, ++i)
+        copy_async16(to + i * NC * 16, ahead + (long long)v * W);
+    copy_commit();
+    block_arrive<2, NT>(); // the row is written
+    sp = sn;
+    n = next;
+  }
+}
+
+// Resident form: rows of at most (NT - 32) * RV accesses.  The next row is on its way into shared memory while this one is
+// worked on in registers.
 template <typename T, int NT, int RV>
 __global__ void __launch_bounds__(NT, 512 / NT) distill_resident_kernel(const DistillArgs a) {
   constexpr int W = 16 / (int)sizeof(T), NC = NT - 32;
@@ -234,34 +353,14 @@ __global__ void __launch_bounds__(NT, 512 / NT) distill_resident_kernel(const Di
   extern __shared__ __align__(16) unsigned char staged[]; // [RV][NC] accesses, then two rows' teachers
   __shared__ Partial red[2]; // rows in turn
   const int tid = threadIdx.x;
-  const float c = a.inv_t * kLog2e;
-  auto row_of = [&](long long n) { return static_cast<const T *>(a.logits) + n * a.logits_stride; };
-  auto weight_of = [&](long long n) { return a.grad_scale * (a.row_weight ? a.row_weight[n] : 1.f); };
-  long long n = blockIdx.x;
-  int turn = 0;
   if (tid >= NC) {
-    unsigned char *const at = staged + NC * RV * 16;
-    bool any = false;
-    float kl = 0.f;
-    if (n < a.rows) kl = read_teacher<T>(a, Teacher(at, a.k), n, row_of(n), any);
-    for (; n < a.rows; n += gridDim.x, turn ^= 1) {
-      const Teacher t(at + turn * teacher_bytes(a.k), a.k);
-      const float wn = weight_of(n);
-      if (tid == NC) red[turn].any = any;
-      block_sync<1, NT>();
-      float m, s;
-      get_partial(red[turn], NC / 32, m, s);
-      const RowScale r = row_scale(a, m, s, wn, any);
-      put_loss(a, n, r, kl, wn, any);
-      const bool put = a.dlogits && any;
-      if (n + gridDim.x < a.rows)
-        kl = read_teacher<T>(a, Teacher(at + (turn ^ 1) * teacher_bytes(a.k), a.k), n + gridDim.x, row_of(n + gridDim.x), any);
-      block_sync<2, NT>();
-      if (put) put_teacher<T>(a, t, static_cast<T *>(a.dlogits) + n * a.grad_stride, r);
-      __syncwarp();
-    }
+    teacher_warp<T, NT>(a, red, staged + NC * RV * 16);
     return;
   }
+  const float c = a.inv_t * kLog2e;
+  auto row_of = [&](long long n) { return static_cast<const T *>(a.logits) + n * a.logits_stride; };
+  long long n = blockIdx.x;
+  int turn = 0;
   const Raw *mine = reinterpret_cast<const Raw *>(staged) + tid;
   const unsigned to = (unsigned)__cvta_generic_to_shared(staged) + tid * 16;
   // the single elements before and after a row's whole accesses: one for each of the first head + tail threads
@@ -280,7 +379,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) distill_resident_kernel(const Di
   if (odd >= 0) load_vec<T, 1>(row_of(n) + odd, single);
   for (; n < a.rows; turn ^= 1) {
     const long long next = n + gridDim.x;
-    const float wn = weight_of(n), one = single[0];
+    const float wn = row_weight_of(a, n), one = single[0];
     const int at = odd;
     copy_wait();
     Raw raw[RV];
@@ -373,7 +472,7 @@ template <typename T, int W> __global__ void __launch_bounds__(kStreamThreads, 2
     __syncthreads();
     get_partial(red, kStreamThreads / 32, m, s);
     const bool any = red.any != 0;
-    const float wn = a.grad_scale * (a.row_weight ? a.row_weight[n] : 1.f);
+    const float wn = row_weight_of(a, n);
     const RowScale r = row_scale(a, m, s, wn, any);
     if (teacher) put_loss(a, n, r, kl, wn, any);
     T *grad = static_cast<T *>(a.dlogits) + n * a.grad_stride;
@@ -419,6 +518,17 @@ template <typename T, int NT> int launch_resident(const DistillArgs &a, int sms,
   distill_resident_kernel<T, NT, kHeld><<<(unsigned)(a.rows < most ? a.rows : most), NT, bytes, s>>>(a);
   return launched();
 }
+constexpr int kMostStaged = 110 * 1024; // bytes of a row and its teachers: two blocks on an SM
+template <typename T, int NT> int launch_staged(const DistillArgs &a, long long accesses, int sms, cudaStream_t s) {
+  const int slots = (int)((accesses + NT - 33) / (NT - 32)), bytes = slots * (NT - 32) * 16 + 2 * teacher_bytes(a.k);
+  static OncePerDevice once;
+  if (!once.get([] { return allow_smem(distill_staged_kernel<T, NT>, kMostStaged); })) return DILOCO_ERR_CUDA;
+  // 64 registers a thread and this shared memory: blocks that an SM holds
+  const int by_smem = (227 * 1024) / (bytes + 2048), per_sm = by_smem < 1024 / NT ? by_smem : 1024 / NT;
+  const long long most = (long long)sms * (per_sm < 1 ? 1 : per_sm);
+  distill_staged_kernel<T, NT><<<(unsigned)(a.rows < most ? a.rows : most), NT, bytes, s>>>(a, slots);
+  return launched();
+}
 template <typename T, int W> int launch_stream(const DistillArgs &a, int sms, cudaStream_t s) {
   distill_stream_kernel<T, W><<<(unsigned)(a.rows < sms * 4ll ? a.rows : sms * 4ll), kStreamThreads, teacher_bytes(a.k), s>>>(a);
   return launched();
@@ -431,9 +541,11 @@ template <typename T> int launch_any(const DistillArgs &a, int sms, cudaStream_t
   const bool same = !a.dlogits || ((x - g) % 16 == 0 && ((a.logits_stride - a.grad_stride) * (long long)sizeof(T)) % 16 == 0);
   if (!same) return launch_stream<T, 1>(a, sms, s);
   const long long n = (a.vocab + W - 1) / W; // accesses of a row
-  if (n <= 32 * kHeld) return launch_resident<T, 64>(a, sms, s);
-  if (n <= 96 * kHeld) return launch_resident<T, 128>(a, sms, s);
-  if (n <= 224 * kHeld) return launch_resident<T, 256>(a, sms, s);
+  // some 12 accesses a thread keep the barrier's share small; two blocks of 512 threads are an SM's registers
+  if (n <= 32 * 12) return launch_staged<T, 64>(a, n, sms, s);
+  if (n <= 96 * 12) return launch_staged<T, 128>(a, n, sms, s);
+  if (n <= 224 * 12) return launch_staged<T, 256>(a, n, sms, s);
+  if ((n + 480) * 16 + 2 * teacher_bytes(a.k) <= kMostStaged) return launch_staged<T, 512>(a, n, sms, s);
   if (n <= 480 * kHeld) return launch_resident<T, 512>(a, sms, s);
   return launch_stream<T, W>(a, sms, s);
 }
