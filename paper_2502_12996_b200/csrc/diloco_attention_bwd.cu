@@ -8,10 +8,12 @@
 //
 // Both loops keep one tile pair in flight and alternate so that the tensor cores work during the exponentials:
 //   dk, dv   tensor cores: dz^T Q of the last tile, V dO^T of this one | P^T dO, K Q^T of the next
-//            256 threads : P^T = exp of this tile                       | dz^T of this tile
+//            the others  : P^T = exp of this tile                       | dz^T of this tile
 //   dq       S of the next tile is under way (two buffers) while dz of this one is formed
-// P and dz stay in tensor memory as bf16, over the columns of S and dP that the same threads have read.  Tiles
-// are 128 x 128; warps 0-3 take the first 64 columns, warps 4-7 the last, one row a thread.  Rows of a partial last
+// P and dz stay in tensor memory as bf16, over the columns of S and dP that the same threads have read.  A block's own
+// tile has 128 rows.  The tiles that it walks have 128 rows with head_dim 128 (256 threads form P and dz, one row
+// and 64 columns each, and a block has an SM's tensor memory to itself), and 64 with head_dim 64 and less (128 threads; two
+// blocks share an SM, so that one's start, waits and end hide behind the other's loop).  Rows of a partial last
 // tile are zeroed in shared memory where they are summed over; a row that comes out non-finite is computed
 // again over the rows it has to do with alone.
 #include <type_traits>
@@ -21,17 +23,25 @@
 namespace diloco {
 namespace {
 
-constexpr int kBwdThreads = 384;
 constexpr int kStages = 2;
 
-template <int HD> struct BwdLayout { // two tiles of the block's own, two rings
-  static constexpr int kPanels = HD / 64, kTileBytes = kPanels * kPanel;
-  static constexpr int kOwn = 0, kRing = 2 * kTileBytes, kStats = kRing + 2 * kStages * kTileBytes;
-  // at least half of an SM's shared memory, so that no second block waits for tensor memory
-  static constexpr int kUsed = kStats + kStages * 2 * kRows * 4 + 1024, kBytes = kUsed > 120 * 1024 ? kUsed : 120 * 1024;
+template <int HD> struct BwdLayout { // two tiles of the block's own, two rings of tiles that it walks
+  static constexpr int kInner = HD == 64 ? 64 : 128, kParts = kInner / 64; // rows of a walked tile, threads of a row
+  static constexpr int kMathWarps = 4 * kParts, kMathThreads = 32 * kMathWarps;
+  static constexpr int kMmaWarp = kMathWarps, kLoadWarp = kMathWarps + 1, kStatWarp = kMathWarps + 2, kThreads = 32 * (kMathWarps + 3);
+  static constexpr int kBlocks = HD == 64 ? 2 : 1, kTmem = 512 / kBlocks; // blocks on an SM
+  static constexpr int kOwnBytes = kRows * HD * 2, kInnerBytes = kInner * HD * 2;
+  static constexpr int kOwn = 0, kRing = 2 * kOwnBytes, kStats = kRing + 2 * kStages * kInnerBytes;
+  // so much of an SM's shared memory that no further block waits for tensor memory
+  static constexpr int kUsed = kStats + kStages * 2 * kInner * 4 + 1024, kLeast = (kBlocks == 1 ? 120 : 80) * 1024;
+  static constexpr int kBytes = kUsed > kLeast ? kUsed : kLeast;
 };
 
-__device__ __forceinline__ void math_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+template <int THREADS> __device__ __forceinline__ void math_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+
+__device__ __forceinline__ void zero_staged(unsigned smem, int r, int columns) {
+  for (int c = 0; c < columns / 4; ++c) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(smem + (c * kRows + r) * 16), "r"(0) : "memory");
+}
 
 // ------------------------------------------------------------------------------------- dq
 struct DqBarriers {
@@ -43,7 +53,7 @@ struct DqBarriers {
 };
 
 template <int HD>
-__global__ void __launch_bounds__(kBwdThreads, 1)
+__global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlocks)
     attn_dq_kernel(const AttnArgs a, const __grid_constant__ HeadMap mq, const __grid_constant__ HeadMap mk, const __grid_constant__ HeadMap mv,
                    const __grid_constant__ HeadMap mdo, int split) {
   using L = BwdLayout<HD>;
@@ -55,20 +65,21 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   if (at.block < 0) {
     if (part != 0) return;
     const int r0 = at.first + (-1 - at.block) * kRows;
-    for (int r = r0 + warp; r < min(r0 + kRows, at.end); r += kBwdThreads / 32) {
+    for (int r = r0 + warp; r < min(r0 + kRows, at.end); r += L::kThreads / 32) {
       for (int c = lane; c < a.head_dim; c += 32) a.dq[r * a.dq_row + h * a.dq_head + c] = __float2bfloat16_rn(0.f);
     }
     return;
   }
   const int q0 = at.first + at.block * kRows;
   if (q0 >= at.end) return;
-  const int all = at.block + 1, tiles = (all - part + split - 1) / split; // this block's key tiles: part, part + split, ...
+  // key tiles, the last of them first; this block's are part, part + split, ...
+  const int all = (min(q0 + kRows, at.end) - at.first + L::kInner - 1) / L::kInner, tiles = (all - part + split - 1) / split;
   const unsigned smem = (smem_u32(raw_smem) + 1023) & ~1023u;
-  const unsigned s_q = smem + L::kOwn, s_do = s_q + L::kTileBytes, s_k = smem + L::kRing, s_v = s_k + kStages * L::kTileBytes;
+  const unsigned s_q = smem + L::kOwn, s_do = s_q + L::kOwnBytes, s_k = smem + L::kRing, s_v = s_k + kStages * L::kInnerBytes;
 
-  if (warp == 8) tmem_alloc(&bar.tmem, 512);
+  if (warp == L::kMmaWarp) tmem_alloc(&bar.tmem, L::kTmem);
   if (threadIdx.x == 0) {
-    mbar_init(&bar.own_full, 1), mbar_init(&bar.dp_full, 1), mbar_init(&bar.ds_full, 256), mbar_init(&bar.o_full, 1);
+    mbar_init(&bar.own_full, 1), mbar_init(&bar.dp_full, 1), mbar_init(&bar.ds_full, L::kMathThreads), mbar_init(&bar.o_full, 1);
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&bar.k_full[i], 1), mbar_init(&bar.v_full[i], 1);
       mbar_init(&bar.k_empty[i], 1), mbar_init(&bar.v_empty[i], 1);
@@ -80,31 +91,31 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  const unsigned tmem = bar.tmem, t_s = tmem, t_dp = tmem + 256, t_dq = tmem + 384;
+  const unsigned tmem = bar.tmem, t_s = tmem, t_dp = tmem + 2 * L::kInner, t_dq = tmem + 3 * L::kInner;
 
-  if (warp >= 8) {
-    if (warp == 9 && lane == 0) {
+  if (warp >= L::kMathWarps) {
+    if (warp == L::kLoadWarp && lane == 0) {
       int issued = 0;
       if (tiles > 0) {
-        mbar_expect_tx(&bar.own_full, 2 * L::kTileBytes);
-        load_tile<HD>(s_q, mq, h, q0, &bar.own_full);
-        load_tile<HD>(s_do, mdo, h, q0, &bar.own_full);
+        mbar_expect_tx(&bar.own_full, 2 * L::kOwnBytes);
+        load_tile<HD, kRows, L::kInner>(s_q, mq, h, q0, &bar.own_full);
+        load_tile<HD, kRows, L::kInner>(s_do, mdo, h, q0, &bar.own_full);
       }
       for (int it = 0; it < tiles; ++it) {
-        const int s = it % kStages, row = at.first + (all - 1 - (it * split + part)) * kRows;
+        const int s = it % kStages, row = at.first + (all - 1 - (it * split + part)) * L::kInner;
         const unsigned ph = ((it / kStages) & 1) ^ 1;
         if (!wait_or_abort(&bar.k_empty[s], ph, &bar.abort)) break;
-        mbar_expect_tx(&bar.k_full[s], L::kTileBytes);
-        load_tile<HD>(s_k + s * L::kTileBytes, mk, g, row, &bar.k_full[s]);
+        mbar_expect_tx(&bar.k_full[s], L::kInnerBytes);
+        load_tile<HD, L::kInner, L::kInner>(s_k + s * L::kInnerBytes, mk, g, row, &bar.k_full[s]);
         issued = 2 * it + 1;
         if (!wait_or_abort(&bar.v_empty[s], ph, &bar.abort)) break;
-        mbar_expect_tx(&bar.v_full[s], L::kTileBytes);
-        load_tile<HD>(s_v + s * L::kTileBytes, mv, g, row, &bar.v_full[s]);
+        mbar_expect_tx(&bar.v_full[s], L::kInnerBytes);
+        load_tile<HD, L::kInner, L::kInner>(s_v + s * L::kInnerBytes, mv, g, row, &bar.v_full[s]);
         issued = 2 * it + 2;
       }
       if (issued < 2 * tiles) land_copies<kStages>(issued, &bar.own_full, bar.k_full, bar.v_full);
-    } else if (warp == 8 && lane == 0 && tiles > 0) {
-      constexpr unsigned kk = mma_desc(128, false, false), kn = mma_desc(HD, false, true);
+    } else if (warp == L::kMmaWarp && lane == 0 && tiles > 0) {
+      constexpr unsigned kk = mma_desc(L::kInner, false, false), kn = mma_desc(HD, false, true);
       bool ok = wait_or_abort(&bar.own_full, 0, &bar.abort) && wait_or_abort(&bar.k_full[0], 0, &bar.abort);
       if (ok) {
         product_ss<HD>(t_s, s_q, s_k, kk);
@@ -123,18 +134,18 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         if (more) {
           ok = wait_or_abort(&bar.k_full[sn], phn, &bar.abort);
           if (!ok) break;
-          product_ss<HD>(t_s + ((it + 1) & 1) * 128, s_q, s_k + sn * L::kTileBytes, kk);
+          product_ss<HD>(t_s + ((it + 1) & 1) * L::kInner, s_q, s_k + sn * L::kInnerBytes, kk);
           mma_commit(&bar.s_full[(it + 1) & 1]);
         }
         ok = wait_or_abort(&bar.ds_full, it & 1, &bar.abort);
         if (!ok) break;
         tmem_fence_after();
-        product_ts(t_dq, t_dp, s_k + s * L::kTileBytes, kn, it > 0);
+        product_ts<L::kInner>(t_dq, t_dp, s_k + s * L::kInnerBytes, kn, it > 0);
         mma_commit(&bar.k_empty[s]);
         if (more) {
           ok = wait_or_abort(&bar.v_full[sn], phn, &bar.abort);
           if (!ok) break;
-          product_ss<HD>(t_dp, s_do, s_v + sn * L::kTileBytes, kk);
+          product_ss<HD>(t_dp, s_do, s_v + sn * L::kInnerBytes, kk);
           mma_commit(&bar.dp_full);
           mma_commit(&bar.v_empty[sn]);
         } else {
@@ -151,13 +162,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     const int half = warp >> 2, r = threadIdx.x & 127, i = q0 + r;
     const bool mine = i < at.end;
     const unsigned lanes = (unsigned)(warp & 3) << 21;
-    // delta: each half of the row's threads sums half of the columns
+    // delta: each of the row's threads sums 64 of the columns
     float delta = 0.f;
     if (mine) {
       const __nv_bfloat16 *x = a.dout + (long long)i * a.do_row + h * a.do_head, *y = a.out_in + (long long)i * a.o_row + h * a.o_head;
 #pragma unroll
-      for (int c = 0; c < HD / 2; c += 8) {
-        const int col = half * (HD / 2) + c;
+      for (int c = 0; c < 64; c += 8) {
+        const int col = half * 64 + c;
         if (col < a.head_dim) {
           float u[8], v[8];
           load_vec<__nv_bfloat16, 8>(x + col, u);
@@ -169,8 +180,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     }
     bar.delta[half][r] = delta;
     if (half == 0) bar.bad[r] = 0;
-    math_sync();
-    delta = bar.delta[0][r] + bar.delta[1][r];
+    math_sync<L::kMathThreads>();
+    delta = L::kParts == 1 ? bar.delta[0][r] : bar.delta[0][r] + bar.delta[1][r];
     const long long stat = (long long)h * a.tokens + i;
     if (mine && half == 0 && part == 0) a.delta[stat] = delta;
     const float lse2 = mine ? a.lse[stat] * kLog2e : 0.f;
@@ -182,7 +193,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       tmem_fence_after();
       unsigned s[2][32];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) tmem_load32(t_s + (it & 1) * 128 + half * 64 + u * 32 + lanes, s[u]);
+      for (int u = 0; u < 2; ++u) tmem_load32(t_s + (it & 1) * L::kInner + half * 64 + u * 32 + lanes, s[u]);
       tmem_wait_load();
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -191,13 +202,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
           const float2 y = fma2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), make_float2(c, c), make_float2(-lse2, -lse2));
           s[u][j] = __float_as_uint(ex2(y.x)), s[u][j + 1] = __float_as_uint(ex2(y.y));
         }
-      const bool diagonal = it == 0 && part == 0;
-      if (diagonal) { // it is the last of the sequence's tiles that this block sees
-        const int valid = at.end - q0; // K rows of it inside the sequence
-        if (valid < kRows) {
-          ok = warp_wait(&bar.k_full[0], 0, &bar.abort);
+      // key `at0` + j of the sequence for query q0 - first + r: hidden behind the diagonal, on the last tiles alone
+      const int at0 = (all - 1 - (it * split + part)) * L::kInner, over = at0 - at.block * kRows;
+      const bool diagonal = over + L::kInner > 0;
+      if (diagonal) {
+        const int valid = at.end - at.first - at0; // K rows of the tile inside the sequence
+        if (valid < L::kInner) {
+          ok = warp_wait(&bar.k_full[it % kStages], (it / kStages) & 1, &bar.abort);
           if (!ok) break;
-          if (r >= valid) zero_row<HD>(s_k, r, half);
+          if (r >= valid && r < L::kInner) zero_row<HD, L::kInner>(s_k + (it % kStages) * L::kInnerBytes, r, half, L::kParts);
           fence_async_smem();
         }
       }
@@ -215,8 +228,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
             float2 y = add2(make_float2(__uint_as_float(d[j]), __uint_as_float(d[j + 1])), make_float2(-delta, -delta));
             y = mul2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), y);
             if (decltype(masked)::value) {
-              if (half * 64 + u * 32 + j > r) y.x = 0.f;
-              if (half * 64 + u * 32 + j + 1 > r) y.y = 0.f;
+              if (over + half * 64 + u * 32 + j > r) y.x = 0.f;
+              if (over + half * 64 + u * 32 + j + 1 > r) y.y = 0.f;
             }
             x[j / 2 % 8] = bf16_pair(y.x, y.y);
             if (j % 16 == 14) tmem_store8(t_dp + half * 64 + u * 16 + j / 16 * 8 + lanes, x);
@@ -231,25 +244,24 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     }
     if (ok && tiles > 0) ok = warp_wait(&bar.o_full, 0, &bar.abort);
     tmem_fence_after();
+    const int c0 = half * 64; // this thread's columns of the accumulator: 64
     if (split == 1) {
       if (ok) {
-        const bool fine = put_row<HD / 2>(t_dq + lanes, a.dq + (long long)i * a.dq_row + h * a.dq_head, half * (HD / 2), a.head_dim, a.scale, mine);
+        const bool fine = put_row<64>(t_dq + lanes, a.dq + (long long)i * a.dq_row + h * a.dq_head, c0, a.head_dim, a.scale, mine);
         if (mine && !fine) bar.bad[r] = 1;
       }
     } else if (ok) {
       // every operand has been read: the tiles' place takes this block's sums
-      if (tiles > 0) stage_row<HD / 2>(t_dq + lanes + half * (HD / 2), smem + half * (HD / 2) * kRows * 4, r);
-      else
-        for (int c = half * (HD / 8); c < (half + 1) * (HD / 8); ++c)
-          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(smem + (c * kRows + r) * 16), "r"(0) : "memory");
+      if (tiles > 0) stage_row<64>(t_dq + lanes + c0, smem + c0 * kRows * 4, r);
+      else zero_staged(smem + c0 * kRows * 4, r, 64);
     }
     if (split == 1) {
-      math_sync(); // both halves are written before a row is written again
+      math_sync<L::kMathThreads>(); // all of a row is written before it is written again
     } else {
       cluster_sync(); // all blocks' sums are staged
-      // eight columns at a time, dealt to the cluster's blocks and both halves
+      // eight columns at a time, dealt to the cluster's blocks and the row's threads
       if (mine && !bar.abort)
-        for (int c = (part * 2 + half) * 8; c < a.head_dim; c += split * 16) {
+        for (int c = (part * L::kParts + half) * 8; c < a.head_dim; c += split * L::kParts * 8) {
           float v[8];
           sum_staged(v, smem, split, c, r);
           if (!put8(a.dq + (long long)i * a.dq_row + h * a.dq_head + c, v, a.scale)) mark_remote(smem_u32(&bar.bad[r]));
@@ -262,9 +274,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   }
   tmem_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == L::kMmaWarp) {
     tmem_fence_after();
-    tmem_free(tmem, 512);
+    tmem_free(tmem, L::kTmem);
   }
   if (threadIdx.x == 0 && bar.abort && a.status) atomicExch(a.status, kStatusTimeout);
 }
@@ -279,7 +291,7 @@ struct DkvBarriers {
 };
 
 template <int HD>
-__global__ void __launch_bounds__(kBwdThreads, 1)
+__global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlocks)
     attn_dkv_kernel(const AttnArgs a, const __grid_constant__ HeadMap mq, const __grid_constant__ HeadMap mk, const __grid_constant__ HeadMap mv,
                     const __grid_constant__ HeadMap mdo, int split) {
   using L = BwdLayout<HD>;
@@ -292,7 +304,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   if (at.block < 0) {
     if (part != 0) return;
     const int r0 = at.first + (-1 - at.block) * kRows;
-    for (int r = r0 + warp; r < min(r0 + kRows, at.end); r += kBwdThreads / 32)
+    for (int r = r0 + warp; r < min(r0 + kRows, at.end); r += L::kThreads / 32)
       for (int c = lane; c < a.head_dim; c += 32) {
         a.dk[r * a.dk_row + g * a.dk_head + c] = __float2bfloat16_rn(0.f);
         a.dv[r * a.dv_row + g * a.dv_head + c] = __float2bfloat16_rn(0.f);
@@ -301,20 +313,20 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   }
   const int k0 = at.first + at.block * kRows; // first key
   if (k0 >= at.end) return;
-  const int per_head = (at.end - k0 + kRows - 1) / kRows, all = per_head * a.group; // query tiles
+  const int per_head = (at.end - k0 + L::kInner - 1) / L::kInner, all = per_head * a.group; // query tiles
   const int tiles = (all - part + split - 1) / split;                              // this block's: part, part + split, ...
   const unsigned smem = (smem_u32(raw_smem) + 1023) & ~1023u;
-  const unsigned s_k = smem + L::kOwn, s_v = s_k + L::kTileBytes, s_q = smem + L::kRing, s_do = s_q + kStages * L::kTileBytes;
+  const unsigned s_k = smem + L::kOwn, s_v = s_k + L::kOwnBytes, s_q = smem + L::kRing, s_do = s_q + kStages * L::kInnerBytes;
   // minus log-sum-exp (times log2 e) and minus delta of a query tile's rows
   float *stats = reinterpret_cast<float *>(raw_smem + (smem - smem_u32(raw_smem)) + L::kStats);
 
-  if (warp == 8) tmem_alloc(&bar.tmem, 512);
+  if (warp == L::kMmaWarp) tmem_alloc(&bar.tmem, L::kTmem);
   if (threadIdx.x == 0) {
     mbar_init(&bar.own_full, 1), mbar_init(&bar.s_full, 1), mbar_init(&bar.dp_full, 1), mbar_init(&bar.o_full, 1);
-    mbar_init(&bar.p_full, 256), mbar_init(&bar.ds_full, 256);
+    mbar_init(&bar.p_full, L::kMathThreads), mbar_init(&bar.ds_full, L::kMathThreads);
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&bar.q_full[i], 1), mbar_init(&bar.do_full[i], 1), mbar_init(&bar.empty[i], 1);
-      mbar_init(&bar.stat_full[i], 32), mbar_init(&bar.stat_empty[i], 256);
+      mbar_init(&bar.stat_full[i], 32), mbar_init(&bar.stat_empty[i], L::kMathThreads);
     }
     bar.abort = 0;
     fence_mbar_init();
@@ -322,43 +334,43 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  const unsigned tmem = bar.tmem, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = t_dv + HD;
+  const unsigned tmem = bar.tmem, t_s = tmem, t_dp = tmem + L::kInner, t_dv = tmem + 2 * L::kInner, t_dk = t_dv + HD;
 
-  if (warp >= 8) {
-    if (warp == 9 && lane == 0) {
+  if (warp >= L::kMathWarps) {
+    if (warp == L::kLoadWarp && lane == 0) {
       int issued = 0;
       if (tiles > 0) {
-        mbar_expect_tx(&bar.own_full, 2 * L::kTileBytes);
-        load_tile<HD>(s_k, mk, g, k0, &bar.own_full);
-        load_tile<HD>(s_v, mv, g, k0, &bar.own_full);
+        mbar_expect_tx(&bar.own_full, 2 * L::kOwnBytes);
+        load_tile<HD, kRows, L::kInner>(s_k, mk, g, k0, &bar.own_full);
+        load_tile<HD, kRows, L::kInner>(s_v, mv, g, k0, &bar.own_full);
       }
       for (int it = 0; it < tiles; ++it) {
-        const int s = it % kStages, n = it * split + part, h = g * a.group + n / per_head, row = k0 + (n % per_head) * kRows;
+        const int s = it % kStages, n = it * split + part, h = g * a.group + n / per_head, row = k0 + (n % per_head) * L::kInner;
         if (!wait_or_abort(&bar.empty[s], ((it / kStages) & 1) ^ 1, &bar.abort)) break;
-        mbar_expect_tx(&bar.q_full[s], L::kTileBytes);
-        load_tile<HD>(s_q + s * L::kTileBytes, mq, h, row, &bar.q_full[s]);
-        mbar_expect_tx(&bar.do_full[s], L::kTileBytes);
-        load_tile<HD>(s_do + s * L::kTileBytes, mdo, h, row, &bar.do_full[s]);
+        mbar_expect_tx(&bar.q_full[s], L::kInnerBytes);
+        load_tile<HD, L::kInner, L::kInner>(s_q + s * L::kInnerBytes, mq, h, row, &bar.q_full[s]);
+        mbar_expect_tx(&bar.do_full[s], L::kInnerBytes);
+        load_tile<HD, L::kInner, L::kInner>(s_do + s * L::kInnerBytes, mdo, h, row, &bar.do_full[s]);
         issued = 2 * it + 2;
       }
       if (issued < 2 * tiles) land_copies<kStages>(issued, &bar.own_full, bar.q_full, bar.do_full);
-    } else if (warp == 10) {
+    } else if (warp == L::kStatWarp) {
       for (int it = 0; it < tiles; ++it) {
-        const int s = it % kStages, n = it * split + part, h = g * a.group + n / per_head, row = k0 + (n % per_head) * kRows;
+        const int s = it % kStages, n = it * split + part, h = g * a.group + n / per_head, row = k0 + (n % per_head) * L::kInner;
         if (!warp_wait(&bar.stat_empty[s], ((it / kStages) & 1) ^ 1, &bar.abort)) break;
-        float *to = stats + s * 2 * kRows;
+        float *to = stats + s * 2 * L::kInner;
 #pragma unroll
-        for (int u = 0; u < kRows / 32; ++u) {
+        for (int u = 0; u < L::kInner / 32; ++u) {
           const int i = row + u * 32 + lane;
           const bool in = i < at.end;
           const long long stat = (long long)h * a.tokens + i;
           to[u * 32 + lane] = in ? -a.lse[stat] * kLog2e : 0.f;
-          to[kRows + u * 32 + lane] = in ? -a.delta[stat] : 0.f;
+          to[L::kInner + u * 32 + lane] = in ? -a.delta[stat] : 0.f;
         }
         mbar_arrive(&bar.stat_full[s]);
       }
-    } else if (warp == 8 && lane == 0 && tiles > 0) {
-      constexpr unsigned kk = mma_desc(128, false, false), kn = mma_desc(HD, false, true);
+    } else if (warp == L::kMmaWarp && lane == 0 && tiles > 0) {
+      constexpr unsigned kk = mma_desc(L::kInner, false, false), kn = mma_desc(HD, false, true);
       bool ok = wait_or_abort(&bar.own_full, 0, &bar.abort) && wait_or_abort(&bar.q_full[0], 0, &bar.abort);
       if (ok) {
         product_ss<HD>(t_s, s_k, s_q, kk);
@@ -376,22 +388,22 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
         ok = wait_or_abort(&bar.p_full, it & 1, &bar.abort);
         if (!ok) break;
         tmem_fence_after();
-        product_ts(t_dv, t_s, s_do + s * L::kTileBytes, kn, it > 0);
+        product_ts<L::kInner>(t_dv, t_s, s_do + s * L::kInnerBytes, kn, it > 0);
         if (more) {
           ok = wait_or_abort(&bar.q_full[sn], phn, &bar.abort);
           if (!ok) break;
-          product_ss<HD>(t_s, s_k, s_q + sn * L::kTileBytes, kk);
+          product_ss<HD>(t_s, s_k, s_q + sn * L::kInnerBytes, kk);
           mma_commit(&bar.s_full);
         }
         ok = wait_or_abort(&bar.ds_full, it & 1, &bar.abort);
         if (!ok) break;
         tmem_fence_after();
-        product_ts(t_dk, t_dp, s_q + s * L::kTileBytes, kn, it > 0);
+        product_ts<L::kInner>(t_dk, t_dp, s_q + s * L::kInnerBytes, kn, it > 0);
         mma_commit(&bar.empty[s]);
         if (more) {
           ok = wait_or_abort(&bar.do_full[sn], phn, &bar.abort);
           if (!ok) break;
-          product_ss<HD>(t_dp, s_v, s_do + sn * L::kTileBytes, kk);
+          product_ss<HD>(t_dp, s_v, s_do + sn * L::kInnerBytes, kk);
           mma_commit(&bar.dp_full);
         } else {
           mma_commit(&bar.o_full);
@@ -413,8 +425,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     for (int it = 0; it < tiles; ++it) {
       const int st = it % kStages, t = (it * split + part) % per_head;
       const unsigned ph = (it / kStages) & 1;
-      const int valid = at.end - (k0 + t * kRows); // query rows of this tile inside the sequence
-      const bool edge = t == 0 || valid < kRows;
+      const int over = t * L::kInner, valid = at.end - k0 - over; // query rows of this tile inside the sequence
+      const bool edge = over < kRows || valid < L::kInner;
       ok = warp_wait(&bar.s_full, it & 1, &bar.abort);
       if (!ok) break;
       tmem_fence_after();
@@ -424,12 +436,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       tmem_wait_load();
       ok = warp_wait(&bar.stat_full[st], ph, &bar.abort);
       if (!ok) break;
-      const float4 *lse = reinterpret_cast<const float4 *>(stats + st * 2 * kRows + half * 64);
-      const float4 *delta = lse + kRows / 4;
+      const float4 *lse = reinterpret_cast<const float4 *>(stats + st * 2 * L::kInner + half * 64);
+      const float4 *delta = lse + L::kInner / 4;
       // query q sees this key from the diagonal on, and there are `valid` queries: masks on the edge tiles alone
       auto hidden = [&](int u, int j) {
         const int q = half * 64 + u * 32 + j;
-        return (t == 0 && q < r) || q >= valid;
+        return over + q < r || q >= valid;
       };
       auto weights = [&](auto masked) {
 #pragma unroll
@@ -453,12 +465,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
       };
       if (edge) weights(std::true_type{});
       else weights(std::false_type{});
-      if (valid < kRows) {
+      if (valid < L::kInner) {
         ok = warp_wait(&bar.q_full[st], ph, &bar.abort) && warp_wait(&bar.do_full[st], ph, &bar.abort);
         if (!ok) break;
-        if (r >= valid) {
-          zero_row<HD>(s_q + st * L::kTileBytes, r, half);
-          zero_row<HD>(s_do + st * L::kTileBytes, r, half);
+        if (r >= valid && r < L::kInner) {
+          zero_row<HD, L::kInner>(s_q + st * L::kInnerBytes, r, half, L::kParts);
+          zero_row<HD, L::kInner>(s_do + st * L::kInnerBytes, r, half, L::kParts);
         }
         fence_async_smem();
       }
@@ -502,29 +514,37 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
     }
     if (ok && tiles > 0) ok = warp_wait(&bar.o_full, 0, &bar.abort);
     tmem_fence_after();
+    const int c0 = half * 64; // this thread's columns of the accumulators: 64
+    __nv_bfloat16 *row_v = a.dv + (long long)j0 * a.dv_row + g * a.dv_head, *row_k = a.dk + (long long)j0 * a.dk_row + g * a.dk_head;
     if (split == 1) {
       if (ok) {
-        bool fine = put_row<HD / 2>(t_dv + lanes, a.dv + (long long)j0 * a.dv_row + g * a.dv_head, half * (HD / 2), a.head_dim, 1.f, mine);
-        fine &= put_row<HD / 2>(t_dk + lanes, a.dk + (long long)j0 * a.dk_row + g * a.dk_head, half * (HD / 2), a.head_dim, a.scale, mine);
+        bool fine = put_row<64>(t_dv + lanes, row_v, c0, a.head_dim, 1.f, mine);
+        fine &= put_row<64>(t_dk + lanes, row_k, c0, a.head_dim, a.scale, mine);
         if (mine && !fine) bar.bad[r] = 1;
       }
     } else if (ok) {
-      // every operand has been read: the tiles' place takes this block's sums, dv by warps 0-3, dk by warps 4-7
-      const unsigned to = smem + half * HD * kRows * 4;
-      if (tiles > 0) stage_row<HD>((half ? t_dk : t_dv) + lanes, to, r);
-      else
-        for (int c = 0; c < HD / 4; ++c) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + (c * kRows + r) * 16), "r"(0) : "memory");
+      // every operand has been read: the tiles' place takes this block's sums, dv and behind it dk
+      const unsigned to = smem + c0 * kRows * 4;
+      if (tiles > 0) {
+        stage_row<64>(t_dv + lanes + c0, to, r);
+        stage_row<64>(t_dk + lanes + c0, to + HD * kRows * 4, r);
+      } else {
+        zero_staged(to, r, 64);
+        zero_staged(to + HD * kRows * 4, r, 64);
+      }
     }
     if (split == 1) {
-      math_sync(); // both halves are written before a row is written again
+      math_sync<L::kMathThreads>(); // all of a row is written before it is written again
     } else {
       cluster_sync(); // all blocks' sums are staged
-      __nv_bfloat16 *row = half ? a.dk + (long long)j0 * a.dk_row + g * a.dk_head : a.dv + (long long)j0 * a.dv_row + g * a.dv_head;
       if (mine && !bar.abort)
-        for (int c = part * 8; c < a.head_dim; c += split * 8) {
+        for (int c = (part * L::kParts + half) * 8; c < a.head_dim; c += split * L::kParts * 8) {
           float v[8];
-          sum_staged(v, smem + half * HD * kRows * 4, split, c, r);
-          if (!put8(row + c, v, half ? a.scale : 1.f)) mark_remote(smem_u32(&bar.bad[r]));
+          sum_staged(v, smem, split, c, r);
+          bool fine = put8(row_v + c, v, 1.f);
+          sum_staged(v, smem + HD * kRows * 4, split, c, r);
+          fine &= put8(row_k + c, v, a.scale);
+          if (!fine) mark_remote(smem_u32(&bar.bad[r]));
         }
       cluster_sync(); // and read: the row is written, and marked in the first block where it is not finite
     }
@@ -534,9 +554,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
   }
   tmem_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == L::kMmaWarp) {
     tmem_fence_after();
-    tmem_free(tmem, 512);
+    tmem_free(tmem, L::kTmem);
   }
   if (threadIdx.x == 0 && bar.abort && a.status) atomicExch(a.status, kStatusTimeout);
 }
@@ -549,20 +569,23 @@ template <int HD> int launch(const AttnArgs &a, const HeadMap &mq, const HeadMap
   cudaGetDevice(&dev);
   const int sms = sm_count(dev);
   const long long ranks = ranks_of(a, kRows);
-  const int by_q = split_of(a, kRows, a.heads, 1, sms), by_k = split_of(a, kRows, a.kv_heads, a.group, sms);
-  const int rc = launch_split(attn_dq_kernel<HD>, ranks * a.heads, by_q, kBwdThreads, bytes, s, false, a, mq, mk, mv, mdo, by_q);
+  using L = BwdLayout<HD>;
+  const int steps = kRows / L::kInner;
+  const int by_q = split_of(a, kRows, a.heads, steps, sms), by_k = split_of(a, kRows, a.kv_heads, a.group * steps, sms);
+  const int rc = launch_split(attn_dq_kernel<HD>, ranks * a.heads, by_q, L::kThreads, bytes, s, false, a, mq, mk, mv, mdo, by_q);
   if (rc != DILOCO_OK) return rc;
-  return launch_split(attn_dkv_kernel<HD>, ranks * a.kv_heads, by_k, kBwdThreads, bytes, s, true, a, mq, mk, mv, mdo, by_k);
+  return launch_split(attn_dkv_kernel<HD>, ranks * a.kv_heads, by_k, L::kThreads, bytes, s, true, a, mq, mk, mv, mdo, by_k);
 }
 
 } // namespace
 
 int attn_backward(const AttnArgs &a, cudaStream_t s) {
   HeadMap mq, mk, mv, mdo;
-  int rc = encode_heads(&mq, a.q, a.head_dim, a.heads, a.q_head, a.tokens, a.q_row, kRows);
-  if (rc == DILOCO_OK) rc = encode_heads(&mk, a.k, a.head_dim, a.kv_heads, a.k_head, a.tokens, a.k_row, kRows);
-  if (rc == DILOCO_OK) rc = encode_heads(&mv, a.v, a.head_dim, a.kv_heads, a.v_head, a.tokens, a.v_row, kRows);
-  if (rc == DILOCO_OK) rc = encode_heads(&mdo, a.dout, a.head_dim, a.heads, a.do_head, a.tokens, a.do_row, kRows);
+  const int box = a.head_dim <= 64 ? BwdLayout<64>::kInner : BwdLayout<128>::kInner;
+  int rc = encode_heads(&mq, a.q, a.head_dim, a.heads, a.q_head, a.tokens, a.q_row, box);
+  if (rc == DILOCO_OK) rc = encode_heads(&mk, a.k, a.head_dim, a.kv_heads, a.k_head, a.tokens, a.k_row, box);
+  if (rc == DILOCO_OK) rc = encode_heads(&mv, a.v, a.head_dim, a.kv_heads, a.v_head, a.tokens, a.v_row, box);
+  if (rc == DILOCO_OK) rc = encode_heads(&mdo, a.dout, a.head_dim, a.heads, a.do_head, a.tokens, a.do_row, box);
   if (rc != DILOCO_OK) return rc;
   return a.head_dim <= 64 ? launch<64>(a, mq, mk, mv, mdo, s) : launch<128>(a, mq, mk, mv, mdo, s);
 }

@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kFwdThreads, 2)
         if (valid < kRows) {
           ok = warp_wait(&bar.v_full[0], 0, &bar.abort);
           if (!ok) break;
-          if (r >= valid) zero_row<HD>(smem + L::kV, r, 0), zero_row<HD>(smem + L::kV, r, 1);
+          if (r >= valid) zero_row<HD>(smem + L::kV, r);
           fence_async_smem();
         }
       }

@@ -198,9 +198,13 @@ int launch_split(void (*kernel)(KArgs...), long long blocks, int split, int thre
   return DILOCO_OK;
 }
 
-template <int HD> __device__ __forceinline__ void load_tile(unsigned smem, const HeadMap &m, int head, int row, unsigned long long *bar) {
+// ROWS rows by boxes of BOX rows, panels of 64 columns one behind the other
+template <int HD, int ROWS = kRows, int BOX = kRows>
+__device__ __forceinline__ void load_tile(unsigned smem, const HeadMap &m, int head, int row, unsigned long long *bar) {
 #pragma unroll
-  for (int p = 0; p < HD / 64; ++p) load_panel(smem + p * kPanel, m, p * 64, head, row, bar);
+  for (int p = 0; p < HD / 64; ++p)
+#pragma unroll
+    for (int b = 0; b < ROWS; b += BOX) load_panel(smem + p * ROWS * 128 + b * 128, m, p * 64, head, row + b, bar);
 }
 
 // Shared memory is not given back under a copy: after a wait that gave up, the loads still in flight of a block's own
@@ -229,20 +233,17 @@ template <int HD> __device__ __forceinline__ void product_ss(unsigned d, unsigne
     mma_ss(d, da + off, db + off, idesc, i > 0);
   }
 }
-// [128 x 128 bf16 in tensor memory: columns 0-63 at a, 64-127 at a + 64] x [128 rows of b], summed over b's rows
-__device__ __forceinline__ void product_ts(unsigned d, unsigned a, unsigned b, unsigned idesc, bool add) {
+// [128 x ROWS bf16 in tensor memory: columns 0-63 at a, 64-127 at a + 64] x [ROWS rows of b], summed over b's rows
+template <int ROWS> __device__ __forceinline__ void product_ts(unsigned d, unsigned a, unsigned b, unsigned idesc, bool add) {
   const unsigned long long db = tile_desc(opaque(b), kPanel);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) mma_ts(d, a + (i / 4) * 64 + (i % 4) * 8, db + i * (2048 / 16), idesc, add || i > 0);
+  for (int i = 0; i < ROWS / 16; ++i) mma_ts(d, a + (i / 4) * 64 + (i % 4) * 8, db + i * (2048 / 16), idesc, add || i > 0);
 }
 
-// Row r of a tile in shared memory; `half` 0 / 1: one half of its bytes
-template <int HD> __device__ __forceinline__ void zero_row(unsigned tile, int r, int half) {
-#pragma unroll
-  for (int p = 0; p < HD / 64; ++p)
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + p * kPanel + r * 128 + (half * 4 + u) * 16), "r"(0) : "memory");
+// Row r of a tile of ROWS rows in shared memory, or one of `parts` equal parts of its bytes
+template <int HD, int ROWS = kRows> __device__ __forceinline__ void zero_row(unsigned tile, int r, int part = 0, int parts = 1) {
+  for (int u = part; u < HD / 8; u += parts)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + (u / 8) * ROWS * 128 + r * 128 + (u % 8) * 16), "r"(0) : "memory");
 }
 
 } // namespace diloco
