@@ -571,7 +571,7 @@ template <int HD> int launch(const AttnArgs &a, const HeadMap &mq, const HeadMap
   const long long ranks = ranks_of(a, kRows);
   using L = BwdLayout<HD>;
   const int steps = kRows / L::kInner;
-  const int by_q = split_of(a, kRows, a.heads, steps, sms), by_k = split_of(a, kRows, a.kv_heads, a.group * steps, sms);
+  const int slots = sms * L::kBlocks, by_q = split_of(a, kRows, a.heads, steps, slots), by_k = split_of(a, kRows, a.kv_heads, a.group * steps, slots);
   const int rc = launch_split(attn_dq_kernel<HD>, ranks * a.heads, by_q, L::kThreads, bytes, s, false, a, mq, mk, mv, mdo, by_q);
   if (rc != DILOCO_OK) return rc;
   return launch_split(attn_dkv_kernel<HD>, ranks * a.kv_heads, by_k, L::kThreads, bytes, s, true, a, mq, mk, mv, mdo, by_k);

@@ -339,7 +339,7 @@ template <int HD> int launch(const AttnArgs &a, const HeadMap &mq, const HeadMap
   if (!once.get([] { return allow_smem(attn_forward_kernel<HD>, FwdLayout<HD>::kBytes); })) return DILOCO_ERR_CUDA;
   int dev = 0;
   cudaGetDevice(&dev);
-  const int split = split_of(a, kRows, a.heads, 1, sm_count(dev));
+  const int split = split_of(a, kRows, a.heads, 1, 2 * sm_count(dev));
   return launch_split(attn_forward_kernel<HD>, ranks_of(a, kRows) * a.heads, split, kFwdThreads, FwdLayout<HD>::kBytes, s, false, a, mq, mk, mv, split,
                       (int)(a.scale < 0.f));
 }

@@ -72,13 +72,15 @@ template <bool FROM_END> __device__ __forceinline__ Place place_of(const AttnArg
 // Ranks that a kernel has to start for every head: all sequences' blocks, the rows behind them, and empty ones.
 inline long long ranks_of(const AttnArgs &a, int rows) { return (long long)a.tokens / rows + a.sequences + 1; }
 
-// How many blocks share one tile's loop (a cluster, 1 to 8): doubled while the tiles do not fill the SMs twice and
-// a tile of average length still leaves every block two steps.
-inline int split_of(const AttnArgs &a, int rows, int heads, int steps_per_row_block, int sms) {
+// How many blocks share one tile's loop (a cluster, 1 to 8): doubled while the tiles do not fill the `slots` (blocks that
+// the SMs hold) and a tile of average length still leaves every block two steps.  (Clusters are dearer to start: two
+// blocks a tile where 264 tiles met 148 slots took 216 us instead of 181, and clusters of two for all ragged calls, the
+// short tiles' second blocks leaving at once, 168 instead of 115.)
+inline int split_of(const AttnArgs &a, int rows, int heads, int steps_per_row_block, int slots) {
   const long long tiles = ((long long)a.tokens / rows + (a.sequences + 1) / 2) * heads;
   const long long steps = (long long)a.tokens / (a.sequences > 0 ? a.sequences : 1) / rows * steps_per_row_block / 2;
   int s = 1;
-  while (s < 8 && tiles * s < 2ll * sms && steps >= 4ll * s) s *= 2;
+  while (s < 8 && tiles * s < slots && steps >= 4ll * s) s *= 2;
   return s;
 }
 
