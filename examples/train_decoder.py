@@ -1,0 +1,192 @@
+"""The inner phase on a real gradient: M replicas of a small decoder (QKNorm, grouped heads, tied embeddings, z-loss)
+trained on packed documents, their gradients formed by the library's operators, stepped by the fused AdamW and joined
+by the eager outer step, all on one GPU.
+
+    python examples/train_decoder.py --phases 4 --inner 20
+
+Every parameter lives in the replicas' flat vectors (theta, bf16 working copy of an fp32 master) and every gradient is
+written in place into the flat gradients that ``State.inner_adamw`` takes; only the matrix products are torch's.  The text
+is synthetic: documents that count upwards with a stride of their own, so that the loss falls from log(vocab) to what the
+first tokens of a document leave open.
+"""
+from __future__ import annotations
+
+import argparse
+import math
+import sys
+from dataclasses import dataclass
+from pathlib import Path
+
+import torch
+
+ROOT = Path(__file__).resolve().parent.parent
+if str(ROOT) not in sys.path:
+    sys.path.insert(0, str(ROOT))
+
+from paper_2502_12996_b200 import binding, inputs, ops  # noqa: E402
+
+
+@dataclass
+class Shape:
+    layers: int = 2
+    d: int = 256
+    heads: int = 4
+    kv_heads: int = 2
+    head_dim: int = 64
+    vocab: int = 1024
+    z_coef: float = 1e-4
+
+
+class Decoder:
+    """Names, offsets and shapes of the parameters in a replica's flat vector, and the two passes."""
+
+    def __init__(self, shape: Shape):
+        self.shape = s = shape
+        qkv, o = (s.heads + 2 * s.kv_heads) * s.head_dim, s.heads * s.head_dim
+        sizes = [("table", (s.vocab, s.d))]
+        for i in range(s.layers):
+            sizes += [(f"{i}.norm1.w", (s.d,)), (f"{i}.norm1.b", (s.d,)), (f"{i}.qkv", (qkv, s.d)), (f"{i}.qnorm", (s.head_dim,)),
+                      (f"{i}.knorm", (s.head_dim,)), (f"{i}.o", (s.d, o)), (f"{i}.norm2.w", (s.d,)), (f"{i}.norm2.b", (s.d,)),
+                      (f"{i}.up", (4 * s.d, s.d)), (f"{i}.down", (s.d, 4 * s.d))]
+        sizes += [("norm.w", (s.d,)), ("norm.b", (s.d,))]
+        self.at, n = {}, 0
+        for name, shp in sizes:
+            self.at[name] = (n, shp)
+            n += (math.prod(shp) + 63) // 64 * 64            # every tensor starts on 128 bytes
+        self.P = n
+
+    def view(self, flat: torch.Tensor, name: str) -> torch.Tensor:
+        """[M, *shape] of one parameter inside [M, stride] (theta or gradients)."""
+        off, shp = self.at[name]
+        return flat[:, off:off + math.prod(shp)].unflatten(1, shp)
+
+    def init(self, flat: torch.Tensor, gen: torch.Generator) -> None:
+        """The same start for every replica."""
+        for name, (off, shp) in self.at.items():
+            v = flat[:, off:off + math.prod(shp)]
+            if name.endswith((".w", "qnorm", "knorm")):
+                v.fill_(1.0)
+            elif not name.endswith(".b"):
+                v.copy_(torch.randn(math.prod(shp), generator=gen, device=flat.device).mul_(0.02 if name == "table" else shp[-1] ** -0.5))
+
+    def forward(self, theta: torch.Tensor, ids: torch.Tensor, cu: torch.Tensor):
+        """ids [M, T], cu: sequences of all replicas' tokens one after another -> (logits [M, T, vocab], what backward needs)."""
+        s, p = self.shape, lambda name: self.view(theta, name)
+        M, T = ids.shape
+        x = ops.embedding_forward(ids, p("table"), scale=math.sqrt(s.d))
+        kept = []
+        for i in range(s.layers):
+            h, m1, r1 = ops.layer_norm_forward(x, p(f"{i}.norm1.w"), p(f"{i}.norm1.b"))
+            qkv = torch.bmm(h, p(f"{i}.qkv").transpose(1, 2)).view(M, T, -1, s.head_dim)
+            q, mq, rq = ops.layer_norm_forward(qkv[:, :, :s.heads], p(f"{i}.qnorm"))
+            k, mk, rk = ops.layer_norm_forward(qkv[:, :, s.heads:s.heads + s.kv_heads], p(f"{i}.knorm"))
+            q, k, v = (t.flatten(0, 1) for t in (q, k, qkv[:, :, s.heads + s.kv_heads:]))
+            a, lse = ops.attention_forward(q, k, v, cu)
+            y = torch.baddbmm(x, a.view(M, T, -1), p(f"{i}.o").transpose(1, 2))
+            g, m2, r2 = ops.layer_norm_forward(y, p(f"{i}.norm2.w"), p(f"{i}.norm2.b"))
+            u = torch.bmm(g, p(f"{i}.up").transpose(1, 2))
+            f = torch.nn.functional.gelu(u)
+            kept.append((x, h, m1, r1, qkv, q, k, v, mq, rq, mk, rk, a, lse, y, g, m2, r2, u, f))
+            x = torch.baddbmm(y, f, p(f"{i}.down").transpose(1, 2))
+        z, m, r = ops.layer_norm_forward(x, p("norm.w"), p("norm.b"))
+        return torch.bmm(z, p("table").transpose(1, 2)), (ids, cu, kept, x, z, m, r)
+
+    def backward(self, theta: torch.Tensor, grads: torch.Tensor, dlogits: torch.Tensor, saved) -> None:
+        """Writes the gradient of every parameter into grads [M, stride]."""
+        s = self.shape
+        p, dp = (lambda name: self.view(theta, name)), (lambda name: self.view(grads, name))
+        ids, cu, kept, x, z, m, r = saved
+        M, T = ids.shape
+        torch.bmm(dlogits.transpose(1, 2), z, out=dp("table"))                     # the table as output projection
+        dx = ops.layer_norm_backward(torch.bmm(dlogits, p("table")), x, p("norm.w"), m, r, dp("norm.w"), dp("norm.b"))
+        for i in reversed(range(s.layers)):
+            x, h, m1, r1, qkv, q, k, v, mq, rq, mk, rk, a, lse, y, g, m2, r2, u, f = kept[i]
+            torch.bmm(dx.transpose(1, 2), f, out=dp(f"{i}.down"))
+            du = torch.ops.aten.gelu_backward(torch.bmm(dx, p(f"{i}.down")), u)
+            torch.bmm(du.transpose(1, 2), g, out=dp(f"{i}.up"))
+            dx += ops.layer_norm_backward(torch.bmm(du, p(f"{i}.up")), y, p(f"{i}.norm2.w"), m2, r2, dp(f"{i}.norm2.w"), dp(f"{i}.norm2.b"))
+            torch.bmm(dx.transpose(1, 2), a.view(M, T, -1), out=dp(f"{i}.o"))
+            da = torch.bmm(dx, p(f"{i}.o")).view(M * T, s.heads, s.head_dim)
+            dqkv = torch.empty_like(qkv)
+            dq, dk, dv = dqkv[:, :, :s.heads], dqkv[:, :, s.heads:s.heads + s.kv_heads], dqkv[:, :, s.heads + s.kv_heads:]
+            ops.attention_backward(da, q, k, v, a, lse, cu, dq=dq.flatten(0, 1), dk=dk.flatten(0, 1), dv=dv.flatten(0, 1))
+            ops.layer_norm_backward(dq, qkv[:, :, :s.heads], p(f"{i}.qnorm"), mq, rq, dp(f"{i}.qnorm"), dx=dq)
+            ops.layer_norm_backward(dk, qkv[:, :, s.heads:s.heads + s.kv_heads], p(f"{i}.knorm"), mk, rk, dp(f"{i}.knorm"), dx=dk)
+            dqkv = dqkv.view(M, T, -1)
+            torch.bmm(dqkv.transpose(1, 2), h, out=dp(f"{i}.qkv"))
+            dx += ops.layer_norm_backward(torch.bmm(dqkv, p(f"{i}.qkv")), x, p(f"{i}.norm1.w"), m1, r1, dp(f"{i}.norm1.w"), dp(f"{i}.norm1.b"))
+        ops.embedding_backward(ids, dx, dp("table"), scale=math.sqrt(s.d), accumulate=True)   # the table as embedding
+
+
+def documents(M: int, T: int, vocab: int, gen: torch.Generator, device):
+    """M rows of T tokens: documents of 20 to 200 tokens that count upwards from a random start with a stride of 1 to 5,
+    the targets (the next token of the document, -1 at its end), and all rows' documents as cu_seqlens."""
+    ids = torch.empty((M, T), dtype=torch.int32)
+    target = torch.full((M, T), -1, dtype=torch.int32)
+    cu = [0]
+    for m in range(M):
+        at = 0
+        while at < T:
+            n = min(T - at, int(torch.randint(20, 201, (), generator=gen)))
+            first, stride = int(torch.randint(0, vocab, (), generator=gen)), int(torch.randint(1, 6, (), generator=gen))
+            doc = (first + stride * torch.arange(n)) % vocab
+            ids[m, at:at + n] = doc
+            target[m, at:at + n - 1] = doc[1:]
+            at += n
+            cu.append(m * T + at)
+    return ids.to(device), target.to(device), torch.tensor(cu, dtype=torch.int32, device=device)
+
+
+def loss_and_gradients(net: Decoder, theta, grads, ids, target, cu):
+    """One forward and backward pass of all replicas; returns each replica's mean loss."""
+    M, T = ids.shape
+    logits, saved = net.forward(theta, ids, cu)
+    flat = logits.view(M * T, -1)
+    weight = (1.0 / (target >= 0).sum(1).clamp_min(1)).float().repeat_interleave(T)
+    loss, _, dlogits = ops.distill_loss(flat, target.view(-1, 1), torch.zeros((M * T, 1), device=ids.device), z_coef=net.shape.z_coef,
+                                        row_weight=weight, dlogits=flat)           # the gradient in place of the logits
+    net.backward(theta, grads, dlogits.view_as(logits), saved)
+    return loss.view(M, T).sum(1)
+
+
+def train(shape: Shape = Shape(), M: int = 2, T: int = 1024, phases: int = 4, inner: int = 20, lr: float = 2e-3, seed: int = 0,
+          device: str = "cuda:0", say=print):
+    """Runs DiLoCo with eager updates on M replicas; returns the mean loss of every inner step."""
+    net = Decoder(shape)
+    dev = torch.device(device)
+    gen, host = inputs.generator(inputs.BASE_SEED + seed, dev), torch.Generator()
+    host.manual_seed(inputs.BASE_SEED + seed)
+    stride = inputs.padded_stride(net.P)
+    f32 = dict(dtype=torch.float32, device=dev)
+    start = torch.zeros((M, stride), **f32)
+    net.init(start, gen)
+    master, theta = start.clone(), start.to(torch.bfloat16)
+    grads = torch.zeros((M, stride), dtype=torch.bfloat16, device=dev)
+    state = binding.State(M=M, P=net.P, stride=stride, theta=theta, master=master, start=start, outer_mom=torch.zeros((M, stride), **f32),
+                          delta_prev_local=torch.zeros((M, stride), **f32), delta_prev_avg=torch.zeros(stride, **f32),
+                          adam_m=torch.zeros((M, stride), **f32), adam_v=torch.zeros((M, stride), **f32), H=inner, outer_lr=0.4,
+                          theta_kind=binding.THETA_MASTER_BF16, grad_kind=binding.GRAD_BF16, have_prev=0)
+    losses = []
+    for phase in range(phases):
+        for _ in range(inner):
+            ids, target, cu = documents(M, T, shape.vocab, host, dev)
+            loss = loss_and_gradients(net, theta, grads, ids, target, cu)
+            state.inner_adamw(grads, lr)
+            losses.append(loss.mean())
+        state.outer_eager()
+        say(f"phase {phase}: loss {float(losses[-inner]):.3f} -> {float(losses[-1]):.3f}")
+    ops.check_device_status(dev)
+    state.close()
+    return [float(v) for v in losses]
+
+
+if __name__ == "__main__":
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--replicas", type=int, default=2)
+    ap.add_argument("--tokens", type=int, default=1024, help="tokens of each replica in a step")
+    ap.add_argument("--phases", type=int, default=4)
+    ap.add_argument("--inner", type=int, default=20, help="inner steps of a phase")
+    ap.add_argument("--lr", type=float, default=2e-3)
+    ap.add_argument("--seed", type=int, default=0)
+    a = ap.parse_args()
+    train(M=a.replicas, T=a.tokens, phases=a.phases, inner=a.inner, lr=a.lr, seed=a.seed)

@@ -1,0 +1,81 @@
+"""The operators together, as a program uses them: the example's decoder against torch's autograd, and a short run of
+inner and outer steps on its gradients."""
+import math
+import sys
+from pathlib import Path
+
+import pytest
+import torch
+
+sys.path.insert(0, str(Path(__file__).resolve().parent.parent / "examples"))
+import train_decoder  # noqa: E402
+
+from paper_2502_12996_b200 import binding, inputs  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def torch_loss(net, w, ids, target, cu):
+    """One replica's mean loss in fp32, `w`: its parameters by name."""
+    s = net.shape
+    T = ids.numel()
+    F = torch.nn.functional
+    seq = torch.bucketize(torch.arange(T, device=DEV), torch.tensor(cu, device=DEV)[1:], right=True)
+    see = (seq[:, None] == seq[None]) & torch.ones((T, T), device=DEV).tril().bool()
+    x = w["table"][ids.long()] * math.sqrt(s.d)
+    for i in range(s.layers):
+        h = F.layer_norm(x, (s.d,), w[f"{i}.norm1.w"], w[f"{i}.norm1.b"])
+        qkv = (h @ w[f"{i}.qkv"].T).view(T, -1, s.head_dim)
+        q = F.layer_norm(qkv[:, :s.heads], (s.head_dim,), w[f"{i}.qnorm"])
+        k = F.layer_norm(qkv[:, s.heads:s.heads + s.kv_heads], (s.head_dim,), w[f"{i}.knorm"]).repeat_interleave(s.heads // s.kv_heads, 1)
+        v = qkv[:, s.heads + s.kv_heads:].repeat_interleave(s.heads // s.kv_heads, 1)
+        z = torch.einsum("ihd,jhd->hij", q, k) / math.sqrt(s.head_dim)
+        a = torch.einsum("hij,jhd->ihd", torch.softmax(z.masked_fill(~see, -math.inf), -1), v)
+        x = x + a.reshape(T, -1) @ w[f"{i}.o"].T
+        g = F.layer_norm(x, (s.d,), w[f"{i}.norm2.w"], w[f"{i}.norm2.b"])
+        x = x + F.gelu(g @ w[f"{i}.up"].T) @ w[f"{i}.down"].T
+    logits = F.layer_norm(x, (s.d,), w["norm.w"], w["norm.b"]) @ w["table"].T
+    keep = target >= 0
+    lse = torch.logsumexp(logits, -1)
+    loss = F.cross_entropy(logits, target.long().clamp_min(0), reduction="none") + s.z_coef * lse * lse
+    return (loss * keep).sum() / keep.sum()
+
+
+def test_gradients_of_the_whole_decoder():
+    """Against autograd in fp32 on the same (bf16) parameters.  Activations and their gradients are rounded to bf16
+    (2^-9 each) at some 12 places a layer on the way: sqrt(24) * 2^-9 = 1 % of a gradient's norm for two layers, bound 4 %."""
+    torch.cuda.set_device(0)
+    net = train_decoder.Decoder(train_decoder.Shape(d=128, vocab=300))
+    M, T = 2, 320
+    gen, host = inputs.generator(3, DEV), torch.Generator()
+    host.manual_seed(3)
+    stride = inputs.padded_stride(net.P)
+    theta = torch.zeros((M, stride), device=DEV)
+    net.init(theta, gen)
+    theta += torch.randn(theta.shape, generator=gen, device=DEV) * 0.02          # replicas differ
+    theta = theta.to(torch.bfloat16)
+    grads = torch.full((M, stride), 5.0, dtype=torch.bfloat16, device=DEV)
+    ids, target, cu = train_decoder.documents(M, T, 300, host, DEV)
+    before = binding.launch_count()
+    loss = train_decoder.loss_and_gradients(net, theta, grads, ids, target, cu)
+    assert binding.launch_count() - before > 20
+    for m in range(M):
+        w = {n: net.view(theta, n)[m].float().requires_grad_() for n in net.at}
+        mine = [c - m * T for c in cu.tolist() if m * T <= c <= (m + 1) * T]
+        want = torch_loss(net, w, ids[m], target[m], mine)
+        assert abs(float(loss[m]) - float(want.detach())) <= 1e-2 * float(want.detach())
+        want.backward()
+        for n in net.at:
+            got, ref = net.view(grads, n)[m].float(), w[n].grad
+            assert float((got - ref).norm()) <= 0.04 * float(ref.norm()) + 1e-6, n
+
+
+def test_inner_and_outer_steps_learn():
+    """Three phases: the loss falls well below log(vocab) = 6.2, in every phase, and the same run twice gives the same losses."""
+    torch.cuda.set_device(0)
+    how = dict(shape=train_decoder.Shape(d=128, vocab=512), M=2, T=512, phases=3, inner=15, say=lambda *_: None)
+    a = train_decoder.train(**how)
+    assert all(math.isfinite(v) for v in a)
+    assert sum(a[-5:]) / 5 < 0.75 * a[0] and a[-1] < a[15]
+    assert a == train_decoder.train(**how)

@@ -85,3 +85,19 @@ def test_null_and_empty(lib):
     assert lib.diloco_attention_forward(ctypes.byref(attention(tokens=0)), *[None] * 7) == 0
     assert lib.diloco_distill_loss(ctypes.byref(distill(rows=0)), *[None] * 8) == 0
     assert lib.diloco_check_status_word(None, None) == 0
+
+
+def test_tensor_layer_refuses_before_it_launches():
+    """The extension module loads without a GPU, and tensors on the CPU are refused with a message (never computed)."""
+    torch = pytest.importorskip("torch")
+    from paper_2502_12996_b200 import ops
+    build.build_library()
+    table, ids = torch.zeros(1, 4, 8), torch.zeros(1, 2, dtype=torch.int32)
+    q = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
+    n0 = binding.launch_count()
+    for call in (lambda: ops.embedding_forward(ids, table), lambda: ops.embedding_backward(ids, torch.zeros(1, 2, 8), table),
+                 lambda: ops.layer_norm_forward(table, torch.ones(1, 8)), lambda: ops.attention_forward(q, q, q, torch.tensor([0, 4], dtype=torch.int32)),
+                 lambda: ops.distill_loss(table[0], torch.zeros(4, 1, dtype=torch.int32), torch.zeros(4, 1))):
+        with pytest.raises(ValueError, match="CUDA tensors are wanted, got one on cpu"):
+            call()
+    assert binding.launch_count() == n0
