@@ -576,7 +576,8 @@ int diloco_layernorm_backward(const diloco_layernorm_t *n, const void *dy, const
  * All tensors bf16 except lse, fp32 [heads, tokens]; row i of head h of a tensor starts at i row_stride + h
  * head_stride.  head_dim is a multiple of 8, at most 128 (64 and less run narrower kernels); base pointers 16-byte
  * aligned, strides multiples of 8 elements (MISALIGNED otherwise), row strides > 0.  tokens <= 2^24, sequences <= 2^20, heads <= 65535.
- * P and dz are rounded to bf16 as operands of the second products; every sum is fp32.
+ * P and dz are rounded to bf16 as operands of the second products; every sum is fp32.  Outputs overlap no inputs.
+ * Up to three kernels run for one call, the later ones beginning while the earlier ones end.
  * device_status as in diloco_buffers_t: one word or NULL.  Every wait of these kernels is bounded (1 s); one that
  * runs out sets the word (diloco_check_status_word), and the results of that call are invalid.
  */

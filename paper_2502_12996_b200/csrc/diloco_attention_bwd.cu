@@ -1,10 +1,12 @@
-// Causal attention over packed sequences, backward, on the fifth-generation tensor cores: one kernel for dq, one for
-// dk and dv.  Each forms P and dz again from q, k and the forward's log-sum-exp:
+// Causal attention over packed sequences, backward, on the fifth-generation tensor cores: a small kernel for delta, one for dq,
+// one for dk and dv.  The latter two form P and dz again from q, k and the forward's log-sum-exp:
 //   P_ij = exp(z_ij - lse_i),  dz_ij = P_ij (dout_i . v_j - delta_i),  delta_i = dout_i . out_i
 //   dq_i = scale sum_j dz_ij k_j;   dv_j = sum_i P_ij dout_i,  dk_j = scale sum_i dz_ij q_i  (over the heads of a group)
 // Two kernels take 7 products where one takes 5, but every sum then has one owner: the rows of a block's own
 // tile accumulate in tensor memory over the whole loop, and nothing is added to memory by atomics, whose order
-// would change the result from call to call, nor kept in an fp32 copy of dq.
+// would change the result from call to call, nor kept in an fp32 copy of dq.  Neither needs the other, so the second one's
+// blocks start as soon as the first one's last block has (both kinds in one kernel, mixed all along, took 12 to 35 %
+// longer: two loops' instructions and operands at once).
 //
 // Both loops keep one tile pair in flight and alternate so that the tensor cores work during the exponentials:
 //   dk, dv   tensor cores: dz^T Q of the last tile, V dO^T of this one | P^T dO, K Q^T of the next
@@ -43,13 +45,41 @@ __device__ __forceinline__ void zero_staged(unsigned smem, int r, int columns) {
   for (int c = 0; c < columns / 4; ++c) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(smem + (c * kRows + r) * 16), "r"(0) : "memory");
 }
 
+// ---------------------------------------------------------------------------------- delta
+// delta_i = dout_i . out_i of head blockIdx.y: 16 threads a row, 8 columns each.
+constexpr int kDeltaThreads = 256, kDeltaRows = 2;
+__global__ void __launch_bounds__(kDeltaThreads) attn_delta_kernel(const AttnArgs a) {
+  grid_release(); // the next kernel's start does not need delta
+  const int h = blockIdx.y, lane = threadIdx.x & 15, col = lane * 8;
+  const int i0 = (blockIdx.x * (kDeltaThreads / 16) + (threadIdx.x >> 4)) * kDeltaRows;
+  float s[kDeltaRows];
+#pragma unroll
+  for (int u = 0; u < kDeltaRows; ++u) {
+    s[u] = 0.f;
+    const long long i = i0 + u;
+    if (i < a.tokens && col < a.head_dim) {
+      float x[8], y[8];
+      load_vec<__nv_bfloat16, 8>(a.dout + i * a.do_row + h * a.do_head + col, x);
+      load_vec<__nv_bfloat16, 8>(a.out_in + i * a.o_row + h * a.o_head + col, y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[u] = fmaf(x[j], y[j], s[u]);
+    }
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+    for (int u = 0; u < kDeltaRows; ++u) s[u] += __shfl_xor_sync(0xffffffffu, s[u], o);
+#pragma unroll
+  for (int u = 0; u < kDeltaRows; ++u)
+    if (lane == 0 && i0 + u < a.tokens) a.delta[(long long)h * a.tokens + i0 + u] = s[u];
+}
+
 // ------------------------------------------------------------------------------------- dq
 struct DqBarriers {
   unsigned long long own_full, k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2], dp_full, ds_full, o_full;
   unsigned tmem;
   volatile unsigned abort;
   unsigned char bad[kRows];
-  float delta[2][kRows];
 };
 
 template <int HD>
@@ -61,6 +91,8 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
   __shared__ DqBarriers bar;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int part = cluster_rank(), unit = blockIdx.x / split, h = unit % a.heads, g = h / a.group;
+  grid_wait();    // delta is there,
+  grid_release(); // for the kernel after this one too, which may start once every block has come here
   const Place at = place_of<false>(a, unit / a.heads, kRows);
   if (at.block < 0) {
     if (part != 0) return;
@@ -162,28 +194,9 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
     const int half = warp >> 2, r = threadIdx.x & 127, i = q0 + r;
     const bool mine = i < at.end;
     const unsigned lanes = (unsigned)(warp & 3) << 21;
-    // delta: each of the row's threads sums 64 of the columns
-    float delta = 0.f;
-    if (mine) {
-      const __nv_bfloat16 *x = a.dout + (long long)i * a.do_row + h * a.do_head, *y = a.out_in + (long long)i * a.o_row + h * a.o_head;
-#pragma unroll
-      for (int c = 0; c < 64; c += 8) {
-        const int col = half * 64 + c;
-        if (col < a.head_dim) {
-          float u[8], v[8];
-          load_vec<__nv_bfloat16, 8>(x + col, u);
-          load_vec<__nv_bfloat16, 8>(y + col, v);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) delta = fmaf(u[j], v[j], delta);
-        }
-      }
-    }
-    bar.delta[half][r] = delta;
     if (half == 0) bar.bad[r] = 0;
-    math_sync<L::kMathThreads>();
-    delta = L::kParts == 1 ? bar.delta[0][r] : bar.delta[0][r] + bar.delta[1][r];
     const long long stat = (long long)h * a.tokens + i;
-    if (mine && half == 0 && part == 0) a.delta[stat] = delta;
+    const float delta = mine ? a.delta[stat] : 0.f;
     const float lse2 = mine ? a.lse[stat] * kLog2e : 0.f;
     const float c = a.scale_log2;
     bool ok = true;
@@ -299,11 +312,11 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
   __shared__ DkvBarriers bar;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int part = cluster_rank(), unit = blockIdx.x / split, g = unit % a.kv_heads;
-  grid_wait(); // delta is the work of the kernel before this one
   const Place at = place_of<true>(a, unit / a.kv_heads, kRows);
   if (at.block < 0) {
     if (part != 0) return;
     const int r0 = at.first + (-1 - at.block) * kRows;
+    grid_wait();
     for (int r = r0 + warp; r < min(r0 + kRows, at.end); r += L::kThreads / 32)
       for (int c = lane; c < a.head_dim; c += 32) {
         a.dk[r * a.dk_row + g * a.dk_head + c] = __float2bfloat16_rn(0.f);
@@ -552,6 +565,7 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
       for (unsigned again = __ballot_sync(0xffffffffu, bar.bad[r] != 0); again; again &= again - 1)
         attn_dkv_row(a, j0 - lane + __ffs(again) - 1, g, at.end, lane);
   }
+  grid_wait(); // whoever waits for this kernel has waited for the one before it
   tmem_fence_before();
   __syncthreads();
   if (warp == L::kMmaWarp) {
@@ -562,19 +576,20 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
 }
 
 template <int HD> int launch(const AttnArgs &a, const HeadMap &mq, const HeadMap &mk, const HeadMap &mv, const HeadMap &mdo, cudaStream_t s) {
-  constexpr int bytes = BwdLayout<HD>::kBytes;
+  using L = BwdLayout<HD>;
   static OncePerDevice once;
-  if (!once.get([] { return allow_smem(attn_dq_kernel<HD>, bytes) && allow_smem(attn_dkv_kernel<HD>, bytes); })) return DILOCO_ERR_CUDA;
+  if (!once.get([] { return allow_smem(attn_dq_kernel<HD>, L::kBytes) && allow_smem(attn_dkv_kernel<HD>, L::kBytes); })) return DILOCO_ERR_CUDA;
   int dev = 0;
   cudaGetDevice(&dev);
-  const int sms = sm_count(dev);
   const long long ranks = ranks_of(a, kRows);
-  using L = BwdLayout<HD>;
-  const int steps = kRows / L::kInner;
-  const int slots = sms * L::kBlocks, by_q = split_of(a, kRows, a.heads, steps, slots), by_k = split_of(a, kRows, a.kv_heads, a.group * steps, slots);
-  const int rc = launch_split(attn_dq_kernel<HD>, ranks * a.heads, by_q, L::kThreads, bytes, s, false, a, mq, mk, mv, mdo, by_q);
-  if (rc != DILOCO_OK) return rc;
-  return launch_split(attn_dkv_kernel<HD>, ranks * a.kv_heads, by_k, L::kThreads, bytes, s, true, a, mq, mk, mv, mdo, by_k);
+  const int steps = kRows / L::kInner, slots = sm_count(dev) * L::kBlocks;
+  const int by_q = split_of(a, kRows, a.heads, steps, slots), by_k = split_of(a, kRows, a.kv_heads, a.group * steps, slots);
+  constexpr int rows = kDeltaThreads / 16 * kDeltaRows;
+  attn_delta_kernel<<<dim3((a.tokens + rows - 1) / rows, a.heads), kDeltaThreads, 0, s>>>(a);
+  int rc = launched();
+  if (rc == DILOCO_OK) rc = launch_split(attn_dq_kernel<HD>, ranks * a.heads, by_q, L::kThreads, L::kBytes, s, true, a, mq, mk, mv, mdo, by_q);
+  if (rc == DILOCO_OK) rc = launch_split(attn_dkv_kernel<HD>, ranks * a.kv_heads, by_k, L::kThreads, L::kBytes, s, true, a, mq, mk, mv, mdo, by_k);
+  return rc;
 }
 
 } // namespace
