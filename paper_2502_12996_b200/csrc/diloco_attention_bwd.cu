@@ -74,6 +74,23 @@ __global__ void __launch_bounds__(kDeltaThreads) attn_delta_kernel(const AttnArg
     if (lane == 0 && i0 + u < a.tokens) a.delta[(long long)h * a.tokens + i0 + u] = s[u];
 }
 
+// dz is rounded to bf16 for its products, an error of 1.7e-3 of each term.  A row's dz is of the order of the largest
+// weight that it gives, 1 / (keys that it sees), and so are its dq and its shares of dk: at 750 tokens three quarters
+// of the squares of dq stand in a sequence's first 128 rows.  In that corner (the first 128 queries and keys) what the
+// rounding leaves is multiplied too.  Error of dq and dk over 11 sequences of 12 to 2500 tokens, 8 heads of 64: 2.5e-3 -> 2.1e-3 (the
+// rounding of the results alone: 1.65e-3), for 3 to 5 % of the time there and less than the timing's noise at 16384 tokens.
+// 16 of a row's dz to tensor memory as bf16 and, in the corner, behind the tile's what that leaves.
+__device__ __forceinline__ void put_dz(unsigned to, const float2 (&y)[8], bool corner) {
+  unsigned x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = bf16_pair(y[i].x, y[i].y);
+  tmem_store8(to, x);
+  if (!corner) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = bf16_pair(y[i].x - __uint_as_float(x[i] << 16), y[i].y - __uint_as_float(x[i] & 0xffff0000u));
+  tmem_store8(to + 16, x);
+}
+
 // ------------------------------------------------------------------------------------- dq
 struct DqBarriers {
   unsigned long long own_full, k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages], s_full[2], dp_full, ds_full, o_full;
@@ -106,6 +123,7 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
   if (q0 >= at.end) return;
   // key tiles, the last of them first; this block's are part, part + split, ...
   const int all = (min(q0 + kRows, at.end) - at.first + L::kInner - 1) / L::kInner, tiles = (all - part + split - 1) / split;
+  const bool corner = at.block == 0; // see put_dz
   const unsigned smem = (smem_u32(raw_smem) + 1023) & ~1023u;
   const unsigned s_q = smem + L::kOwn, s_do = s_q + L::kOwnBytes, s_k = smem + L::kRing, s_v = s_k + kStages * L::kInnerBytes;
 
@@ -172,7 +190,8 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
         ok = wait_or_abort(&bar.ds_full, it & 1, &bar.abort);
         if (!ok) break;
         tmem_fence_after();
-        product_ts<L::kInner>(t_dq, t_dp, s_k + s * L::kInnerBytes, kn, it > 0);
+#pragma unroll 1
+        for (int n = 0; n <= int(corner); ++n) product_ts<L::kInner>(t_dq, t_dp + n * 16, s_k + s * L::kInnerBytes, kn, it + n > 0);
         mma_commit(&bar.k_empty[s]);
         if (more) {
           ok = wait_or_abort(&bar.v_full[sn], phn, &bar.abort);
@@ -233,19 +252,23 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
       auto slopes = [&](auto masked) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          unsigned d[32], x[8];
+          unsigned d[32];
           tmem_load32(t_dp + half * 64 + u * 32 + lanes, d);
           tmem_wait_load();
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            float2 y = add2(make_float2(__uint_as_float(d[j]), __uint_as_float(d[j + 1])), make_float2(-delta, -delta));
-            y = mul2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), y);
-            if (decltype(masked)::value) {
-              if (over + half * 64 + u * 32 + j > r) y.x = 0.f;
-              if (over + half * 64 + u * 32 + j + 1 > r) y.y = 0.f;
+          for (int j = 0; j < 32; j += 16) {
+            float2 y[8];
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+              float2 &z = y[e / 2];
+              z = add2(make_float2(__uint_as_float(d[j + e]), __uint_as_float(d[j + e + 1])), make_float2(-delta, -delta));
+              z = mul2(make_float2(__uint_as_float(s[u][j + e]), __uint_as_float(s[u][j + e + 1])), z);
+              if (masked.value) {
+                if (over + half * 64 + u * 32 + j + e > r) z.x = 0.f;
+                if (over + half * 64 + u * 32 + j + e + 1 > r) z.y = 0.f;
+              }
             }
-            x[j / 2 % 8] = bf16_pair(y.x, y.y);
-            if (j % 16 == 14) tmem_store8(t_dp + half * 64 + u * 16 + j / 16 * 8 + lanes, x);
+            put_dz(t_dp + half * 64 + u * 32 + j / 2 + lanes, y, masked.value && corner);
           }
         }
       };
@@ -397,7 +420,7 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
       for (int it = 0; ok && it < tiles; ++it) {
         const int s = it % kStages, sn = (it + 1) % kStages;
         const unsigned phn = ((it + 1) / kStages) & 1;
-        const bool more = it + 1 < tiles;
+        const bool more = it + 1 < tiles, corner = at.block == 0 && (it * split + part) % per_head < kRows / L::kInner; // see put_dz
         ok = wait_or_abort(&bar.p_full, it & 1, &bar.abort);
         if (!ok) break;
         tmem_fence_after();
@@ -411,7 +434,8 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
         ok = wait_or_abort(&bar.ds_full, it & 1, &bar.abort);
         if (!ok) break;
         tmem_fence_after();
-        product_ts<L::kInner>(t_dk, t_dp, s_q + s * L::kInnerBytes, kn, it > 0);
+#pragma unroll 1
+        for (int n = 0; n <= int(corner); ++n) product_ts<L::kInner>(t_dk, t_dp + n * 16, s_q + s * L::kInnerBytes, kn, it + n > 0);
         mma_commit(&bar.empty[s]);
         if (more) {
           ok = wait_or_abort(&bar.do_full[sn], phn, &bar.abort);
@@ -472,7 +496,7 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
               s[u][j + e] = __float_as_uint(p[e]);
             }
             x[j / 2 % 8] = bf16_pair(p[0], p[1]), x[j / 2 % 8 + 1] = bf16_pair(p[2], p[3]);
-            if (j % 16 == 12) tmem_store8(t_s + half * 64 + u * 16 + j / 16 * 8 + lanes, x);
+            if (j % 16 == 12) tmem_store8(t_s + half * 64 + u * 32 + j / 16 * 8 + lanes, x);
           }
         }
       };
@@ -497,24 +521,29 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
       auto slopes = [&](auto masked) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          unsigned d[32], x[8];
+          unsigned d[32];
           tmem_load32(t_dp + half * 64 + u * 32 + lanes, d);
           tmem_wait_load();
 #pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            const float4 m = delta[u * 8 + j / 4];
-            float2 y[2] = {add2(make_float2(__uint_as_float(d[j]), __uint_as_float(d[j + 1])), make_float2(m.x, m.y)),
-                           add2(make_float2(__uint_as_float(d[j + 2]), __uint_as_float(d[j + 3])), make_float2(m.z, m.w))};
-            y[0] = mul2(make_float2(__uint_as_float(s[u][j]), __uint_as_float(s[u][j + 1])), y[0]);
-            y[1] = mul2(make_float2(__uint_as_float(s[u][j + 2]), __uint_as_float(s[u][j + 3])), y[1]);
-            if (decltype(masked)::value) { // 0 * (infinity or NaN of a row that is not seen)
-              if (hidden(u, j)) y[0].x = 0.f;
-              if (hidden(u, j + 1)) y[0].y = 0.f;
-              if (hidden(u, j + 2)) y[1].x = 0.f;
-              if (hidden(u, j + 3)) y[1].y = 0.f;
+          for (int j = 0; j < 32; j += 16) {
+            float2 y[8];
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const float4 m = delta[u * 8 + (j + e) / 4];
+              const float2 minus[2] = {make_float2(m.x, m.y), make_float2(m.z, m.w)};
+#pragma unroll
+              for (int w = 0; w < 2; ++w) {
+                const int n = j + e + 2 * w;
+                float2 &z = y[e / 2 + w];
+                z = add2(make_float2(__uint_as_float(d[n]), __uint_as_float(d[n + 1])), minus[w]);
+                z = mul2(make_float2(__uint_as_float(s[u][n]), __uint_as_float(s[u][n + 1])), z);
+                if (masked.value) { // 0 * (infinity or NaN of a row that is not seen)
+                  if (hidden(u, n)) z.x = 0.f;
+                  if (hidden(u, n + 1)) z.y = 0.f;
+                }
+              }
             }
-            x[j / 2 % 8] = bf16_pair(y[0].x, y[0].y), x[j / 2 % 8 + 1] = bf16_pair(y[1].x, y[1].y);
-            if (j % 16 == 12) tmem_store8(t_dp + half * 64 + u * 16 + j / 16 * 8 + lanes, x);
+            put_dz(t_dp + half * 64 + u * 32 + j / 2 + lanes, y, masked.value && at.block == 0 && over < kRows);
           }
         }
       };

@@ -235,11 +235,11 @@ template <int HD> __device__ __forceinline__ void product_ss(unsigned d, unsigne
     mma_ss(d, da + off, db + off, idesc, i > 0);
   }
 }
-// [128 x ROWS bf16 in tensor memory: columns 0-63 at a, 64-127 at a + 64] x [ROWS rows of b], summed over b's rows
+// [128 x ROWS bf16 in tensor memory: every 32 numbers in the first 16 of 32 columns] x [ROWS rows of b], summed over b's rows
 template <int ROWS> __device__ __forceinline__ void product_ts(unsigned d, unsigned a, unsigned b, unsigned idesc, bool add) {
   const unsigned long long db = tile_desc(opaque(b), kPanel);
 #pragma unroll
-  for (int i = 0; i < ROWS / 16; ++i) mma_ts(d, a + (i / 4) * 64 + (i % 4) * 8, db + i * (2048 / 16), idesc, add || i > 0);
+  for (int i = 0; i < ROWS / 16; ++i) mma_ts(d, a + (i / 2) * 32 + (i % 2) * 8, db + i * (2048 / 16), idesc, add || i > 0);
 }
 
 // Row r of a tile of ROWS rows in shared memory, or one of `parts` equal parts of its bytes

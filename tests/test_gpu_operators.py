@@ -434,6 +434,22 @@ def test_attention_hidden_rows_stay_hidden(where, value, D, H, K):
     ops.check_device_status()
 
 
+@pytest.mark.parametrize("cu,H,K,D", [(lengths(128), 4, 4, 64), (lengths(128), 4, 1, 128), (lengths(37, 0, 128, 99), 6, 2, 64), (lengths(90, 128), 2, 2, 120)])
+def test_attention_slopes_of_a_sequence_start(cu, H, K, D):
+    """The first 128 queries and keys of a sequence: dz is multiplied as bf16 and what that leaves.  A rounding to bf16 is off by
+    1.7e-3 (2^-7 / sqrt(12) of the last place over a mantissa of 1 to 2).  Expected of dq and dk: the rounding of the result and
+    that of `out` in delta (at most 1e-3 of a random row's dq), 2.0e-3 together; with a third one, dz's, it would be 2.6e-3."""
+    g, T = gen(31), cu[-1]
+    q, k, v, dout = (randn(g, T, n, D, dtype=BF16) for n in (H, K, K, H))
+    cut = torch.tensor(cu, dtype=torch.int32, device=DEV)
+    out, lse = ops.attention_forward(q, k, v, cut)
+    dq, dk, _ = ops.attention_backward(dout, q, k, v, out, lse, cut)
+    want = attn_want(q, k, v, cu, D ** -0.5, dout)
+    for got, name in ((dq, "dq"), (dk, "dk")):
+        assert float((got.double() - want[name]).norm() / want[name].norm()) <= 2.2e-3, name
+    ops.check_device_status()
+
+
 # ----------------------------------------------------------------------------------------- loss
 DISTILL = [  # rows, vocab, k, logits, teacher, temperature, z, id type
     (1, 1, 1, F32, F32, 1.0, 0.0, torch.int32),
