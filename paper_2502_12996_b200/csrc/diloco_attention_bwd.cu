@@ -47,38 +47,131 @@ __device__ __forceinline__ void zero_staged(unsigned smem, int r, int columns) {
 
 // ---------------------------------------------------------------------------------- delta
 // delta_i = dout_i . out_i of head blockIdx.y: 16 threads a row, 8 columns each.
-constexpr int kDeltaThreads = 256, kDeltaRows = 2;
-__global__ void __launch_bounds__(kDeltaThreads) attn_delta_kernel(const AttnArgs a) {
-  grid_release(); // the next kernel's start does not need delta
-  const int h = blockIdx.y, lane = threadIdx.x & 15, col = lane * 8;
-  const int i0 = (blockIdx.x * (kDeltaThreads / 16) + (threadIdx.x >> 4)) * kDeltaRows;
-  float s[kDeltaRows];
+//
+// `out` is rounded to bf16, and where a row has few keys (or one dominant weight) dz is small beside that: over sequences of two
+// tokens dq would be off by 4.0e-3, of four by 2.8e-3, of 16 by 2.2e-3, where the rounding of dq itself is 1.65e-3.  So the first
+// 16 rows of every sequence take delta_i = sum_j P_ij (dout_i . v_j) from their own 16 keys: one warp a sequence and head, 64 columns'
+// loads at once, q k^T and dout v^T as small matrix instructions.  It costs about 1 us of the whole backward (300 tokens, 8 heads of
+// 64: 15.4 -> 16.8 us), one launch with the other rows; 64 of those a block keep enough loads on their way for 114 registers.
+constexpr int kDeltaThreads = 256, kDeltaRows = 4, kFirst = 16;
+constexpr int kDeltaBlock = kDeltaThreads / 16 * kDeltaRows; // rows of a block
+
+// 16 x 8 += 16 x 16 times 16 x 8, a warp's: of a the rows lane / 4 and 8 below, of b the column lane / 4, of both four numbers of the axis
+// that is summed over: any four, as long as every lane with the same lane % 4 has the same ones
+__device__ __forceinline__ void mma_16x8(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The first rows of the sequence [first, end) for head h.
+__device__ __forceinline__ void first_deltas(const AttnArgs &a, int first, int end, int h) {
+  const int lane = threadIdx.x & 31, row = lane >> 2, two = (lane & 3) * 2, n = min(end - first, kFirst), g = h / a.group;
+  const bool in[2] = {row < n, row + 8 < n};
+  float lse2[2]; // of this thread's two rows
 #pragma unroll
-  for (int u = 0; u < kDeltaRows; ++u) {
-    s[u] = 0.f;
-    const long long i = i0 + u;
-    if (i < a.tokens && col < a.head_dim) {
-      float x[8], y[8];
-      load_vec<__nv_bfloat16, 8>(a.dout + i * a.do_row + h * a.do_head + col, x);
-      load_vec<__nv_bfloat16, 8>(a.out_in + i * a.o_row + h * a.o_head + col, y);
+  for (int w = 0; w < 2; ++w) lse2[w] = in[w] ? a.lse[(long long)h * a.tokens + first + row + 8 * w] * kLog2e : 0.f;
+  float s[2][4] = {}, dp[2][4] = {}; // by key: the first 8, the last 8
+#pragma unroll 1
+  for (int c = (lane & 3) * 16; c - (lane & 3) * 16 < a.head_dim; c += 64) {
+    unsigned x[4][2][8]; // of q, k, dout, v: the two rows' 16 columns from c on
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[u] = fmaf(x[j], y[j], s[u]);
-    }
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const bool there = in[w] && c + 8 * e < a.head_dim;
+        const long long i = first + row + 8 * w;
+        const __nv_bfloat16 *p[4] = {a.q + i * a.q_row + h * a.q_head, a.k + i * a.k_row + g * a.k_head, a.dout + i * a.do_row + h * a.do_head,
+                                     a.v + i * a.v_row + g * a.v_head};
+#pragma unroll
+        for (int o = 0; o < 4; ++o) {
+          const uint4 y = there ? *reinterpret_cast<const uint4 *>(p[o] + c + 8 * e) : make_uint4(0, 0, 0, 0);
+          x[o][w][4 * e] = y.x, x[o][w][4 * e + 1] = y.y, x[o][w][4 * e + 2] = y.z, x[o][w][4 * e + 3] = y.w;
+        }
+      }
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        mma_16x8(s[u], x[0][0][e], x[0][1][e], x[0][0][e + 1], x[0][1][e + 1], x[1][u][e], x[1][u][e + 1]);
+        mma_16x8(dp[u], x[2][0][e], x[2][1][e], x[2][0][e + 1], x[2][1][e + 1], x[3][u][e], x[3][u][e + 1]);
+      }
   }
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1)
+  for (int w = 0; w < 2; ++w) {
+    const int i = row + 8 * w;
+    float sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < kDeltaRows; ++u) s[u] += __shfl_xor_sync(0xffffffffu, s[u], o);
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-  for (int u = 0; u < kDeltaRows; ++u)
-    if (lane == 0 && i0 + u < a.tokens) a.delta[(long long)h * a.tokens + i0 + u] = s[u];
+      for (int e = 0; e < 2; ++e)
+        if (u * 8 + two + e <= i) sum = fmaf(ex2(fmaf(s[u][2 * w + e], a.scale_log2, -lse2[w])), dp[u][2 * w + e], sum);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    if (two == 0 && in[w]) a.delta[(long long)h * a.tokens + first + i] = sum;
+  }
+}
+
+// The first blocks take the sequences' first rows, the others the rest of 64 rows each.
+__global__ void __launch_bounds__(kDeltaThreads) attn_delta_kernel(const AttnArgs a, int first_blocks) {
+  __shared__ int starts[kDeltaBlock + kFirst], ends[kDeltaBlock + kFirst], count;
+  grid_release(); // the next kernel waits where it needs delta
+  const int h = blockIdx.y;
+  if ((int)blockIdx.x < first_blocks) {
+    const int b = blockIdx.x * (kDeltaThreads / 32) + (threadIdx.x >> 5);
+    if (b < a.sequences) first_deltas(a, max(a.cu[b], 0), min(a.cu[b + 1], a.tokens), h);
+    return;
+  }
+  const int lane = threadIdx.x & 15, col = lane * 8, base = (blockIdx.x - first_blocks) * kDeltaBlock;
+  const int i0 = base + (threadIdx.x >> 4) * kDeltaRows;
+  uint4 x[kDeltaRows] = {}, y[kDeltaRows] = {};
+#pragma unroll
+  for (int u = 0; u < kDeltaRows; ++u) {
+    const long long i = i0 + u;
+    if (i < a.tokens && col < a.head_dim) {
+      x[u] = *reinterpret_cast<const uint4 *>(a.dout + i * a.do_row + h * a.do_head + col);
+      y[u] = *reinterpret_cast<const uint4 *>(a.out_in + i * a.o_row + h * a.o_head + col);
+    }
+  }
+  // sequences whose first rows reach into this block's: from a place near them where there are many, else all are looked at
+  if (threadIdx.x == 0) count = 0;
+  __syncthreads();
+  int b0 = 0;
+  for (int hi = a.sequences > 1024 ? a.sequences : 0; b0 < hi;) {
+    const int mid = (b0 + hi) >> 1;
+    if (a.cu[mid] > base - kFirst) hi = mid;
+    else b0 = mid + 1;
+  }
+  for (int b = b0 + threadIdx.x; b < a.sequences; b += kDeltaThreads) {
+    const int first = a.cu[b], end = a.cu[b + 1];
+    if (first >= base + kDeltaBlock) break;
+    if (first <= base - kFirst || first >= end) continue;
+    const int at = atomicAdd(&count, 1); // in any order: they have no row in common
+    if (at < kDeltaBlock + kFirst) starts[at] = first, ends[at] = min(first + kFirst, end);
+  }
+  __syncthreads();
+  const int listed = min(count, kDeltaBlock + kFirst);
+#pragma unroll
+  for (int u = 0; u < kDeltaRows; ++u) {
+    float p[8], r[8], s = 0.f;
+    unpack(x[u], p);
+    unpack(y[u], r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fmaf(p[j], r[j], s);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    bool mine = lane == 0 && i0 + u < a.tokens;
+    for (int n = 0; n < listed; ++n) mine = mine && (i0 + u < starts[n] || i0 + u >= ends[n]);
+    if (mine) a.delta[(long long)h * a.tokens + i0 + u] = s;
+  }
 }
 
 // dz is rounded to bf16 for its products, an error of 1.7e-3 of each term.  A row's dz is of the order of the largest
 // weight that it gives, 1 / (keys that it sees), and so are its dq and its shares of dk: at 750 tokens three quarters
 // of the squares of dq stand in a sequence's first 128 rows.  In that corner (the first 128 queries and keys) what the
-// rounding leaves is multiplied too.  Error of dq and dk over 11 sequences of 12 to 2500 tokens, 8 heads of 64: 2.5e-3 -> 2.1e-3 (the
-// rounding of the results alone: 1.65e-3), for 3 to 5 % of the time there and less than the timing's noise at 16384 tokens.
+// rounding leaves is multiplied too.  Error of dq and dk over 11 sequences of 12 to 2500 tokens, 8 heads of 64, with the first rows' delta:
+// 2.5e-3 -> 2.0e-3 (the rounding of the results alone: 1.65e-3), for 3 % of the time there and less than the timing's noise at
+// 16384 tokens.
 // 16 of a row's dz to tensor memory as bf16 and, in the corner, behind the tile's what that leaves.
 __device__ __forceinline__ void put_dz(unsigned to, const float2 (&y)[8], bool corner) {
   unsigned x[8];
@@ -108,10 +201,11 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
   __shared__ DqBarriers bar;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int part = cluster_rank(), unit = blockIdx.x / split, h = unit % a.heads, g = h / a.group;
-  grid_wait();    // delta is there,
-  grid_release(); // for the kernel after this one too, which may start once every block has come here
+  // delta is waited for where it is first needed, and only then may the kernel after this one start, which reads it too (one
+  // thread's release counts for its block)
   const Place at = place_of<false>(a, unit / a.heads, kRows);
   if (at.block < 0) {
+    grid_wait();
     if (part != 0) return;
     const int r0 = at.first + (-1 - at.block) * kRows;
     for (int r = r0 + warp; r < min(r0 + kRows, at.end); r += L::kThreads / 32) {
@@ -120,7 +214,10 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
     return;
   }
   const int q0 = at.first + at.block * kRows;
-  if (q0 >= at.end) return;
+  if (q0 >= at.end) {
+    grid_wait();
+    return;
+  }
   // key tiles, the last of them first; this block's are part, part + split, ...
   const int all = (min(q0 + kRows, at.end) - at.first + L::kInner - 1) / L::kInner, tiles = (all - part + split - 1) / split;
   const bool corner = at.block == 0; // see put_dz
@@ -215,6 +312,8 @@ __global__ void __launch_bounds__(BwdLayout<HD>::kThreads, BwdLayout<HD>::kBlock
     const unsigned lanes = (unsigned)(warp & 3) << 21;
     if (half == 0) bar.bad[r] = 0;
     const long long stat = (long long)h * a.tokens + i;
+    grid_wait();
+    grid_release();
     const float delta = mine ? a.delta[stat] : 0.f;
     const float lse2 = mine ? a.lse[stat] * kLog2e : 0.f;
     const float c = a.scale_log2;
@@ -613,8 +712,8 @@ template <int HD> int launch(const AttnArgs &a, const HeadMap &mq, const HeadMap
   const long long ranks = ranks_of(a, kRows);
   const int steps = kRows / L::kInner, slots = sm_count(dev) * L::kBlocks;
   const int by_q = split_of(a, kRows, a.heads, steps, slots), by_k = split_of(a, kRows, a.kv_heads, a.group * steps, slots);
-  constexpr int rows = kDeltaThreads / 16 * kDeltaRows;
-  attn_delta_kernel<<<dim3((a.tokens + rows - 1) / rows, a.heads), kDeltaThreads, 0, s>>>(a);
+  const int first_blocks = (a.sequences + kDeltaThreads / 32 - 1) / (kDeltaThreads / 32);
+  attn_delta_kernel<<<dim3(first_blocks + (a.tokens + kDeltaBlock - 1) / kDeltaBlock, a.heads), kDeltaThreads, 0, s>>>(a, first_blocks);
   int rc = launched();
   if (rc == DILOCO_OK) rc = launch_split(attn_dq_kernel<HD>, ranks * a.heads, by_q, L::kThreads, L::kBytes, s, true, a, mq, mk, mv, mdo, by_q);
   if (rc == DILOCO_OK) rc = launch_split(attn_dkv_kernel<HD>, ranks * a.kv_heads, by_k, L::kThreads, L::kBytes, s, true, a, mq, mk, mv, mdo, by_k);

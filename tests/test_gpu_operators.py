@@ -450,6 +450,41 @@ def test_attention_slopes_of_a_sequence_start(cu, H, K, D):
     ops.check_device_status()
 
 
+@pytest.mark.parametrize("n,count,H,K,D", [(2, 40, 4, 4, 64), (3, 50, 4, 2, 128), (7, 33, 3, 1, 72), (16, 9, 2, 2, 128), (1, 70, 2, 1, 64)])
+def test_attention_short_sequences(n, count, H, K, D):
+    """Sequences of n tokens, between empty ones: nothing but the rounding of the result to bf16 is left in dq and dk (1.7e-3), for
+    dz is small beside the rounding of `out` in delta = dout . out (4e-3 of dq at two tokens).  A sequence of one token has dz = 0."""
+    g, cu = gen(37), lengths(*([n, 0] * count))
+    T = cu[-1]
+    q, k, v, dout = (randn(g, T, m, D, dtype=BF16) for m in (H, K, K, H))
+    cut = torch.tensor(cu, dtype=torch.int32, device=DEV)
+    out, lse = ops.attention_forward(q, k, v, cut)
+    dq, dk, _ = ops.attention_backward(dout, q, k, v, out, lse, cut)
+    want = attn_want(q, k, v, cu, D ** -0.5, dout)
+    for got, name in ((dq, "dq"), (dk, "dk")):
+        if n == 1:                                            # dout . v twice, in fp32 by two orders of sums
+            assert float(got.double().abs().max()) <= 64 * U32 * float(want[name + "_s"].max()), name
+        else:
+            assert float((got.double() - want[name]).norm() / want[name].norm()) <= 1.9e-3, name
+    ops.check_device_status()
+
+
+def test_attention_delta_of_many_sequences():
+    """More sequences than one look goes through, of lengths about a block's rows."""
+    g = gen(41)
+    n = torch.randint(0, 9, (2500,), generator=g, device=DEV).tolist()
+    n[::400] = [40] * len(n[::400])
+    cu, T = lengths(*n), sum(n)
+    q, k, v, dout = (randn(g, T, m, 64, dtype=BF16) for m in (2, 1, 1, 2))
+    cut = torch.tensor(cu, dtype=torch.int32, device=DEV)
+    out, lse = ops.attention_forward(q, k, v, cut)
+    dq, dk, _ = ops.attention_backward(dout, q, k, v, out, lse, cut)
+    want = attn_want(q, k, v, cu, 0.125, dout)
+    for got, name in ((dq, "dq"), (dk, "dk")):
+        assert float((got.double() - want[name]).norm() / want[name].norm()) <= 1.9e-3, name
+    ops.check_device_status()
+
+
 # ----------------------------------------------------------------------------------------- loss
 DISTILL = [  # rows, vocab, k, logits, teacher, temperature, z, id type
     (1, 1, 1, F32, F32, 1.0, 0.0, torch.int32),
