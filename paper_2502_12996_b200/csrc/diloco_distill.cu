@@ -10,8 +10,10 @@
 //   staged    two rows fit an SM's shared memory (up to 110 KB): a block keeps one there; sum of exponentials and gradient
 //             read it from there, and each piece of the next row is on its way as soon as the gradient has read this
 //             one's.  Two or more blocks on an SM, so that one's exponentials (the special-function unit's 16 a cycle, twice an
-//             element, take 3/4 of the time that the row's bytes take) run beside another's loads and stores.
-//   resident  one row fits a block's registers (up to 138 KB): the row is in registers and the next one in shared memory
+//             element, take 3/4 of the time that the row's bytes take) run beside another's loads and stores.  16384 x 50021
+//             bf16, 64 entries: 624 us, 5.25 TB/s of logits and gradient; fp32 rows of 80 KB 5.9 TB/s (in registers 5.1)
+//   resident  one row fits a block's registers (up to 138 KB): the row is in registers and the next one in shared memory.
+//             8192 x 32000 fp32: 341 us, 6.15 TB/s
 //   stream    longer rows are read twice, the second time mostly from L2
 // One warp of the block has the teacher's entries and nothing else: their fetch, softmax and share of the loss, and the
 // elements of the gradient that they touch, are as long a chain of small steps as the row itself.  Rows need not start on
@@ -256,7 +258,12 @@ template <typename T, int NT> __device__ __forceinline__ void teacher_warp(const
 }
 
 // Staged form.  NT - 32 threads for the row, `slots` accesses each at most; every thread copies what it will itself read, so
-// one barrier a row is enough, the one for the sums of all warps.
+// one barrier a row is enough, the one for the sums of all warps.  A row comes in quarters (four accesses a thread; 16 hold the longest
+// row), and its sum begins with the first of them (all of the row waited for: 16384 x 50021 bf16 655 us instead of 624).
+constexpr int kQuarters = 4;
+template <typename F> __device__ __forceinline__ void each_quarter(F f) {
+  f(std::integral_constant<int, 0>{}), f(std::integral_constant<int, 1>{}), f(std::integral_constant<int, 2>{}), f(std::integral_constant<int, 3>{});
+}
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT) distill_staged_kernel(const DistillArgs a, int slots) {
   constexpr int W = 16 / (int)sizeof(T), NC = NT - 32;
@@ -277,8 +284,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_staged_kernel(const Dis
   // the single elements before and after a row's whole accesses: one for each of the first head + tail threads
   auto odd_of = [&](const Span &sp) { return tid < sp.head ? tid : tid < sp.head + sp.tail ? sp.body * W + tid : -1; };
   Span sp = span_of<T, W>(row_of(n), a.vocab);
-  for (int v = tid, i = 0; v < sp.body; v += NC, ++i) copy_async16(to + i * NC * 16, row_of(n) + sp.head + (long long)v * W);
-  copy_commit();
+  for (int q = 0; q < kQuarters; ++q) {
+    for (int i = 4 * q, v = tid + i * NC; i < 4 * q + 4 && v < sp.body; v += NC, ++i)
+      copy_async16(to + i * NC * 16, row_of(n) + sp.head + (long long)v * W);
+    copy_commit();
+  }
   int odd = odd_of(sp);
   float single[1] = {-INFINITY};
   if (odd >= 0) load_vec<T, 1>(row_of(n) + odd, single);
@@ -286,25 +296,29 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_staged_kernel(const Dis
     const long long next = n + gridDim.x;
     const float wn = row_weight_of(a, n), one = single[0];
     const int at = odd, head = sp.head, body = sp.body;
-    copy_wait();
-    // running maximum and sum, two accesses at a time
+    // running maximum and sum, four accesses at a time as they come in
     float m = one * c, m0 = m == -INFINITY ? 0.f : m; // nothing but -infinity (or no element): every term is 0
     const float2 cc = make_float2(c, c);
     float2 sum = make_float2(at >= 0 ? ex2(fmaf(one, c, -m0)) : 0.f, 0.f);
-#pragma unroll 2
-    for (int v = tid, i = 0; v < body; v += 2 * NC, i += 2) {
-      const bool both = v + NC < body;
-      const Raw x = mine[i * NC], y = mine[(both ? i + 1 : i) * NC];
-      const float top = fmaxf(pack_max(x), pack_max(y)) * c;
+    each_quarter([&](auto quarter) {
+      constexpr int q = decltype(quarter)::value;
+      copy_wait<kQuarters - 1 - q>();
+      const int v = tid + 4 * q * NC;
+      if (v >= body) return;
+      Raw x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = mine[(4 * q + (v + u * NC < body ? u : 0)) * NC];
+      const float top = fmaxf(fmaxf(pack_max(x[0]), pack_max(x[1])), fmaxf(pack_max(x[2]), pack_max(x[3]))) * c;
       if (top > m) {
         const float f = m == -INFINITY ? 1.f : ex2(m - top); // -infinity so far: the sum is 0 (or NaN)
         sum = mul2(sum, make_float2(f, f));
         m = m0 = top;
       }
       const float2 mm = make_float2(-m0, -m0);
-      add_terms(x, cc, mm, sum);
-      if (both) add_terms(y, cc, mm, sum);
-    }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (v + u * NC < body) add_terms(x[u], cc, mm, sum);
+    });
     put_partial(red[turn], m, sum.x + sum.y);
     Span sn = sp;
     single[0] = -INFINITY;
@@ -315,29 +329,33 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_staged_kernel(const Dis
     }
     block_sync<1, NT>();
     const T *ahead = row_of(next) + sn.head;
+    const int coming = next < a.rows ? sn.body : 0, most = max(a.dlogits ? body : 0, coming);
+    RowScale r = {};
     if (a.dlogits) {
       float s;
       get_partial(red[turn], NC / 32, m, s);
-      const RowScale r = row_scale(a, m, s, wn, red[turn].any != 0);
-      T *grad = static_cast<T *>(a.dlogits) + n * a.grad_stride;
-      const float2 lse2 = make_float2(-r.lse2, -r.lse2), coef = make_float2(r.coef, r.coef);
-      Raw *out = reinterpret_cast<Raw *>(grad + head);
-#pragma unroll 4
-      for (int v = tid, i = 0; v < body; v += NC, ++i) {
+      r = row_scale(a, m, s, wn, red[turn].any != 0);
+    }
+    T *grad = static_cast<T *>(a.dlogits) + n * a.grad_stride;
+    const float2 lse2 = make_float2(-r.lse2, -r.lse2), coef = make_float2(r.coef, r.coef);
+    Raw *out = reinterpret_cast<Raw *>(grad + head);
+#pragma unroll 1
+    for (int q = 0; q < kQuarters; ++q) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = 4 * q + u, v = tid + i * NC;
+        if (v >= most) break;
         const Raw x = mine[i * NC];
         const Raw g = terms(x, cc, lse2, coef);
-        if (next < a.rows && v < sn.body) copy_async16(to + i * NC * 16, ahead + (long long)v * W); // x has been used
-        out[v] = g;
+        if (v < coming) copy_async16(to + i * NC * 16, ahead + (long long)v * W); // x has been used
+        if (a.dlogits && v < body) out[v] = g;
       }
-      if (at >= 0) {
-        const float x[1] = {term(one, c, r)};
-        store_vec<T, 1>(grad + at, x);
-      }
+      copy_commit();
     }
-    if (next < a.rows) // what this row had no place for, or all of it
-      for (int i = a.dlogits ? (body - tid + NC - 1) / NC : 0, v = tid + i * NC; v < sn.body; v += NC, ++i)
-        copy_async16(to + i * NC * 16, ahead + (long long)v * W);
-    copy_commit();
+    if (a.dlogits && at >= 0) {
+      const float x[1] = {term(one, c, r)};
+      store_vec<T, 1>(grad + at, x);
+    }
     block_arrive<2, NT>(); // the row is written
     sp = sn;
     n = next;
@@ -519,6 +537,7 @@ template <typename T, int NT> int launch_resident(const DistillArgs &a, int sms,
   return launched();
 }
 constexpr int kMostStaged = 110 * 1024; // bytes of a row and its teachers: two blocks on an SM
+static_assert(kMostStaged / 16 / 480 <= 4 * kQuarters, "accesses of a thread");
 template <typename T, int NT> int launch_staged(const DistillArgs &a, long long accesses, int sms, cudaStream_t s) {
   const int slots = (int)((accesses + NT - 33) / (NT - 32)), bytes = slots * (NT - 32) * 16 + 2 * teacher_bytes(a.k);
   static OncePerDevice once;
