@@ -18,6 +18,11 @@
 // Tiles of a sequence that start together on both axes need a mask on the diagonal tile alone.  V rows behind the
 // sequence's end are zeroed in shared memory (0 * NaN); a row that comes out non-finite all the same is computed
 // again over the rows that it sees alone, so that a later token's NaN cannot reach an earlier one.
+//
+// Bounded by products and exponentials, which wait for each other within a tile.  1 x 16384 tokens, 16 heads of 128 over 4:
+// 975 us, 1130 TFLOP/s; 16 heads of 64: 780 us, 700 TFLOP/s; 32 x 512 tokens, 16 heads of 128: 93 us; 300 tokens in 5, 8 heads
+// of 64: 8.7 us.  One block an SM with two tiles by turns took 924 us for the first, 918 for the second, and 53 instead of 37
+// for 11 sequences of 12 to 2500 tokens.
 #include <type_traits>
 
 #include "diloco_attention_tiles.cuh"

@@ -1,6 +1,6 @@
 // Scaled embedding lookup and its gradient by sorted tokens, for M replicas in one launch each.
 //
-// Forward: out[m, t] = scale * table[m, ids[m, t]], a gather of rows: memory alone bounds it.
+// Forward: out[m, t] = scale * table[m, ids[m, t]], a gather of rows: memory alone bounds it.  2 x 32768 rows of 2048 bf16: 62 us.
 //
 // Backward: dtable[m, v] = scale * sum_{t: ids[m, t] = v} dout[m, t].  The bytes it cannot do without are
 // dout once and, unless it accumulates, the whole of dtable once (most rows zero: a text uses a part of the
@@ -16,6 +16,10 @@
 //              that crosses chunks leaves fp32 partial sums
 //   4 join     runs that cross chunks (the second launch lists them): partial sums in chunk order
 // Sums run in token order inside a chunk, then in chunk order: a fixed order for given ids.
+//
+// 2 x 32768 tokens, 32000 x 2048 bf16: 131 us for the 530 MB that it reads and writes at least (4.1 TB/s), the sums 67 of them; 4 x 8192
+// tokens, 32000 x 512, fp32 gradients: 71 us, 33 of them the zeros.  Zeroing in the third launch, evenly among its blocks, made
+// these 138 and 80 us; 16 columns a thread instead of 8 made the first 199.
 #include <type_traits>
 
 #include "diloco_ops.cuh"
@@ -464,11 +468,14 @@ int lanes_for(int d, int vw) {
 }
 
 // Tokens of one chunk: 32, twice as many (up to 256) as long as the SMs still get two rounds of chunks: every run that crosses
-// chunks costs the join a chain of loads, and every chunk up to two rows of partial sums.
+// chunks costs the join a chain of loads, and every chunk up to two rows of partial sums.  Half as many (down to 8) while the chunks
+// do not fill half of the SMs' places: 32 rows one after another take 11 us however few there are (2 x 1800 tokens of width 1000:
+// 28.8 -> 24.7 us for the whole call, 8 x 138 of 1280: 49.4 -> 43.9).
 int chunk_for(const diloco_embedding_t *e) {
   const int64_t lanes = lanes_for(e->d, 8), round = 148 * 3 * kWorkThreads; // threads of a round, three blocks an SM
   int c = 32;
   while (c < 256 && e->tokens * e->M * lanes / (2 * c) >= 2 * round) c *= 2;
+  while (c > 8 && e->tokens * e->M * lanes / c < round / 2) c /= 2;
   return c;
 }
 
